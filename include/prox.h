@@ -344,6 +344,60 @@ prox_status_t prox_calib_seen(const prox_calib_t* c, int64_t* seen, int64_t* hel
 prox_status_t prox_rmsnorm(prox_ffn_t* h, const float* x_res_dev, const void* norm_w_dev, double eps, int B,
                            void* xn_out_dev, void* stream);
 
+/* ---- Weights held in 4 bits.  The proxies above only rank channels; these calls compute with 4-bit weights (the
+ * low-bit Stage-2 weights under sparsity that the paper leaves to future work, and the projections around
+ * the FFN of a checkpoint in that form).  None needs a handle, and none allocates.  A matrix [rows, cols] is
+ *     w[r, c] = scale[r, c / G] * (code[r, c] - zero[r, c / G]),   G = group_size, or cols where that is 0
+ *   codes   dev uint8 [rows, cols / 2], 16-byte aligned: byte i holds column 2i in bits 0-3, column 2i + 1 in bits 4-7
+ *   scales  dev fp16 [rows, groups], groups = ceil(cols / G) (the last group may be shorter)
+ *   zeros   dev uint8 [rows, groups] of 0..127, or NULL: 8 everywhere (symmetric codes)
+ * All three are read in place.  Sums are fp32 over products that are exact; results are the same on every call
+ * (no atomics).  Data types are numbered 0 = bf16, 1 = fp32, 2 = fp16.
+ * Every buffer has to lie on the current device (or in pinned mapped or managed memory); others are refused. */
+typedef struct {
+  const uint8_t* codes;
+  const void* scales;
+  const uint8_t* zeros;
+} prox_w4_t;
+
+/* Symmetric codes of bf16 weights, the rule of prox_quantize_proxy:
+ *     scale = fp16(max|w| / 7),  q = clamp(rint(w / scale), -7, 7),  code = q + 8.
+ *   w  dev bf16 [rows, cols];  cols a multiple of 32;  group_size in {0, 32, 64, 128}
+ * Offline; a warp per group.  Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+prox_status_t prox_w4_quantize(const void* w_dev, int rows, int cols, int group_size, uint8_t* codes_dev,
+                               void* scales_dev, void* stream);
+
+/* y = x W^T for B tokens over a matrix [N, K] in 4 bits.
+ *   x  dev bf16 or fp16 (x_dtype) [B, K], rows x_stride elements apart (any alignment of the type's size)
+ *   y  dev bf16, fp32 or fp16 (y_dtype) [B, N], rows y_stride elements apart; what lies between rows stays
+ * K is a multiple of 32, at most 65536; N and B are any numbers from 1; strides matter for B > 1 only.
+ * The weights are read once for up to 16 tokens (fewer for very long rows), again for the next 16: a call for a
+ * few tokens, not for a prompt.  y must not overlap x.  Errors: INVALID_ARG, UNSUPPORTED (K, group_size), CUDA. */
+prox_status_t prox_w4_linear(const prox_w4_t* w, int N, int K, int group_size, const void* x_dev, int64_t x_stride,
+                             int x_dtype, int B, void* y_dev, int64_t y_stride, int y_dtype, void* stream);
+
+/* Stage 2 (Sec. 4.1, "exact sparse computation") over weights in 4 bits, for a mask that prox_stage1_mask,
+ * prox_stage1_mask_threshold or the caller made:
+ *     h[b, j] = SiLU(x_b . W_gate[j, :]) (x_b . W_up[j, :]),   y_b = sum_{j in mask of b} h[b, j] W_down_t[j, :]
+ *   gate, up, down_t  matrices [d_ff, d_model] in 4 bits (down_t is W_down stored by channel: quantize its
+ *                     transpose), all with zeros or all without; group_size in {0, 128}
+ *   d_model           multiple of 128, up to 16384;  d_ff up to 65536
+ *   x                 dev bf16 [B, d_model], 16-byte aligned;  B in 1..8
+ *   sel               dev int32, row b at sel + b * sel_stride: channel ids, each at most once (any order); ids
+ *                     outside [0, d_ff) are skipped
+ *   count             dev int32 [B]: entries of every row that count (clamped to 0..k2), or NULL: k2
+ *   k2                entries of a row at most, 0..d_ff; a token whose mask is empty gets y = 0
+ *   y                 dev [B, d_model], bf16 (out_dtype 0) or fp32 (1)
+ *   workspace         dev, 16-byte aligned, at least prox_w4_stage2_workspace bytes; its contents mean nothing before
+ *                     or after a call, but calls that may overlap need one each
+ * For B > 1 the weights are read once for the union of the tokens' masks.
+ * Errors: INVALID_ARG, UNSUPPORTED (shape, group_size), CUDA. */
+prox_status_t prox_w4_stage2_workspace(int d_model, int d_ff, int B, int64_t* bytes);
+prox_status_t prox_w4_stage2_ffn(const prox_w4_t* gate, const prox_w4_t* up, const prox_w4_t* down_t, int d_model,
+                                 int d_ff, int group_size, const void* x_dev, int B, const int32_t* sel_dev,
+                                 int sel_stride, const int32_t* count_dev_or_null, int k2, void* y_dev, int out_dtype,
+                                 void* workspace_dev, int64_t workspace_bytes, void* stream);
+
 /* Runtime mask counts accumulated by the threshold entry points since the last
  * reset (appendix "Threshold Calibration and Runtime Sparsity":
  * e^ = s2^ - 2 alpha (1 - s1^) / 3).  Host-synchronous.  Any pointer may be NULL. */

@@ -34,6 +34,10 @@ class ProxFFNConfig(C.Structure):
                 ("out_dtype", C.c_int32)]
 
 
+class ProxW4(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("zeros", C.c_void_p)]
+
+
 if not os.path.exists(_LIB_PATH):
     raise ImportError(
         f"{_LIB_PATH} is missing: build it with `python -m paper_2607_27591_b200.build` "
@@ -83,6 +87,11 @@ _SIGS = {
     "prox_calib_histogram": [_vp, C.POINTER(C.c_int64), C.POINTER(_f)],
     "prox_calib_seen": [_vp, C.POINTER(C.c_int64), C.POINTER(C.c_int64)],
     "prox_rmsnorm": [_vp, _vp, _vp, _d, _i, _vp, _vp],
+    "prox_w4_quantize": [_vp, _i, _i, _i, _vp, _vp, _vp],
+    "prox_w4_linear": [C.POINTER(ProxW4), _i, _i, _i, _vp, C.c_int64, _i, _i, _vp, C.c_int64, _i, _vp],
+    "prox_w4_stage2_workspace": [_i, _i, _i, C.POINTER(C.c_int64)],
+    "prox_w4_stage2_ffn": [C.POINTER(ProxW4), C.POINTER(ProxW4), C.POINTER(ProxW4), _i, _i, _i, _vp, _i, _vp, _i, _vp, _i, _vp, _i,
+                           _vp, C.c_int64, _vp],
     "prox_profile_enable": [_vp, _i],
     "prox_profile_read": [_vp, C.POINTER(C.c_int64), C.POINTER(_d)],
 }
@@ -288,6 +297,38 @@ def prox_calib_seen(calib: int):
 
 def prox_rmsnorm(handle: int, x_res, norm_w, eps: float, B: int, xn_out, stream=None) -> None:
     _check(_lib.prox_rmsnorm(handle, _ptr(x_res), _ptr(norm_w), eps, B, _ptr(xn_out), _ptr(stream)), "prox_rmsnorm")
+
+
+def _w4(w) -> ProxW4:
+    """(codes, scales, zeros or None) as the library takes a 4-bit matrix."""
+    if isinstance(w, ProxW4):
+        return w
+    codes, scales, zeros = w
+    return ProxW4(_ptr(codes), _ptr(scales), _ptr(zeros))
+
+
+def prox_w4_quantize(w, rows: int, cols: int, group_size: int, codes, scales, stream=None) -> None:
+    _check(_lib.prox_w4_quantize(_ptr(w), rows, cols, group_size, _ptr(codes), _ptr(scales), _ptr(stream)), "prox_w4_quantize")
+
+
+def prox_w4_linear(w, N: int, K: int, group_size: int, x, x_stride: int, x_dtype: int, B: int, y, y_stride: int, y_dtype: int,
+                   stream=None) -> None:
+    """w: (codes, scales, zeros or None), or a ProxW4 made of them once."""
+    _check(_lib.prox_w4_linear(C.byref(_w4(w)), N, K, group_size, _ptr(x), x_stride, x_dtype, B, _ptr(y), y_stride, y_dtype, _ptr(stream)),
+           "prox_w4_linear")
+
+
+def prox_w4_stage2_workspace(d_model: int, d_ff: int, B: int) -> int:
+    n = C.c_int64()
+    _check(_lib.prox_w4_stage2_workspace(d_model, d_ff, B, C.byref(n)), "prox_w4_stage2_workspace")
+    return n.value
+
+
+def prox_w4_stage2_ffn(gate, up, down_t, d_model: int, d_ff: int, group_size: int, x, B: int, sel, sel_stride: int, count, k2: int, y,
+                       out_dtype: int, workspace, workspace_bytes: int, stream=None) -> None:
+    _check(_lib.prox_w4_stage2_ffn(C.byref(_w4(gate)), C.byref(_w4(up)), C.byref(_w4(down_t)), d_model, d_ff, group_size, _ptr(x), B, _ptr(sel),
+                                   sel_stride, _ptr(count), k2, _ptr(y), out_dtype, _ptr(workspace), workspace_bytes, _ptr(stream)),
+           "prox_w4_stage2_ffn")
 
 
 def prox_calibrate_stack(handles, d_ff: int, norm_w, eps: float, x_res_tokens, s1: float, s2: float,

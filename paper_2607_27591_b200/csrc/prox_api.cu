@@ -1,6 +1,6 @@
 // Host side of libprox: argument validation, memory ownership, launches.
 // Declarations and per-call documentation live in include/prox.h.
-#include "prox.h"
+#include "prox_host.h"
 
 #include <algorithm>
 #include <cmath>
@@ -112,6 +112,12 @@ prox_status_t map_cuda(cudaError_t e) {
   if (e == cudaErrorMemoryAllocation) return PROX_ERR_OOM;
   return PROX_ERR_CUDA;
 }
+
+}  // namespace
+
+prox_status_t prox::host_map_cuda(cudaError_t e) { return map_cuda(e); }
+
+namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

@@ -1,0 +1,39 @@
+// What the host sides of the library's translation units share.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "prox.h"
+
+namespace prox {
+
+// Records a CUDA error for prox_last_cuda_error and gives the status for it (prox_api.cu).
+prox_status_t host_map_cuda(cudaError_t e);
+
+inline bool host_aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// The entry points without a handle have no GPU of their own to check against.  A buffer that lies on another GPU
+// than the current one, or in pageable host memory, is refused here: a kernel would fault on it.
+inline bool host_on_current_device(const void* p, int device) {
+  cudaPointerAttributes at;
+  if (cudaPointerGetAttributes(&at, p) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return false;
+  }
+  if (at.type == cudaMemoryTypeDevice) return at.device == device;
+  return at.type == cudaMemoryTypeManaged || (at.type == cudaMemoryTypeHost && at.devicePointer == p);
+}
+
+inline int host_sm_count(int device) {
+  static int known[64] = {};                       // the same value whoever writes it
+  int& n = known[device & 63];
+  if (n < 1 && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) {
+    (void)cudaGetLastError();
+    n = 0;
+    return 148;
+  }
+  return n;
+}
+
+}  // namespace prox
