@@ -36,4 +36,28 @@ inline int host_sm_count(int device) {
   return n;
 }
 
+constexpr int kMaxBlockSmem = 227 * 1024;
+
+// A launch that may be set up while its predecessor on the stream still runs (the kernel waits for it before it reads
+// anything), of clusters of `cluster` blocks.
+template <auto Kern, typename... Args>
+cudaError_t host_launch(int device, unsigned grid, int block, size_t smem, int cluster, cudaStream_t st, Args... args) {
+  static bool allowed[64] = {};                    // per device: more dynamic shared memory than the default has been asked for
+  if (!allowed[device & 63]) {
+    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(Kern), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               kMaxBlockSmem - 1024);
+    if (e != cudaSuccess) return e;
+    allowed[device & 63] = true;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid); cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  cfg.attrs = at; cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, Kern, args...);
+}
+
 }  // namespace prox

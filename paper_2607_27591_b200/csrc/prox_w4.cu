@@ -8,68 +8,53 @@ using namespace prox;
 
 namespace {
 
-constexpr int kMaxSmem = 227 * 1024;
-constexpr int kMaxTokens = 16;           // tokens of one pass over the weights of prox_w4_linear
+constexpr int kMaxSmem = kMaxBlockSmem - 1024;   // dynamic; the kernels have a few words of their own
 constexpr int kFfnTokens = 8;            // tokens of a call of the sparse FFN, as everywhere in the library
-
-template <typename... KArgs>
-cudaError_t launch(void (*kern)(KArgs...), int grid, int block, size_t smem, int cluster, cudaStream_t st, KArgs... args) {
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-  }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid); cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = st;
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
-  cfg.attrs = at; cfg.numAttrs = cluster > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kern, args...);
-}
 
 // Shape of a launch of rows_kernel for `tiles` tiles of 16 rows.
 struct RowsPlan { int S, WM, WK, R, grid; size_t smem; };
 
-int floor_pow2(int v) { int p = 1; while (2 * p <= v) p *= 2; return p; }
-
-RowsPlan plan_rows(int tiles, int K, int B, int nt, int sms) {
-  RowsPlan p;
+// The shape that is done first, in cycles: an SM takes about 35 for 128 columns of a tile when all its warps are busy (10
+// more for every 8 columns of digits), a warp alone 150; the end of a unit costs 400, less where no warp waits for another, the
+// cluster's sum 1800; a token's digits are made at 4 inputs a cycle.
+RowsPlan plan_rows(int tiles, int K, int B, int words, int nt, bool zp, int sms) {
   const int C = (K + 127) / 128;
-  auto fixed = [&](int R, int WM) { return (size_t)2 * w4::kRowWarps * nt * 512 + (size_t)R * WM * 64 * B; };
-  // the tokens have to fit; then columns are split over a cluster while that brings more SMs in
-  int S = 1;
-  while (S < 8 && (size_t)((C + S - 1) / S) * 256 * B + fixed(4, 16) > (size_t)kMaxSmem) S *= 2;
-  while (S < 8 && tiles * S * 2 <= sms && C >= 2 * S) S *= 2;
-  const int Cs = (C + S - 1) / S;
-  p.S = S;
-  p.WK = std::min(w4::kRowWarps, floor_pow2(Cs));
-  p.WM = w4::kRowWarps / p.WK;
-  while (p.WM > 1 && ((tiles + p.WM - 1) / p.WM) * S < sms) p.WM /= 2;
-  const int units = (tiles + p.WM - 1) / p.WM, clusters = std::max(1, std::min(units, sms / S));
-  p.grid = clusters * S;
-  const int mine = (units + clusters - 1) / clusters;
-  p.R = 1;
-  if (S > 1)
-    while (p.R < mine && (size_t)Cs * 256 * B + fixed(p.R + 1, p.WM) <= (size_t)kMaxSmem && p.R < 16) ++p.R;
-  p.smem = (size_t)Cs * 256 * B + fixed(S > 1 ? p.R : 0, p.WM);
-  return p;
+  RowsPlan best = {};
+  double least = 1e30;
+  for (int S = 1; S <= 8; S *= 2) {
+    const int Cs = w4::rows_share(C, S);
+    if (S > 1 && Cs * (S - 1) >= C) break;                   // a block without columns
+    for (int WK = 1; WK <= w4::kRowWarps && WK <= 2 * Cs - 1; WK *= 2)
+      for (int WM = w4::kRowWarps / WK; WM >= 1; WM /= 2) {
+        const size_t sum = S > 1 ? (size_t)WM * 64 * B : 0;  // a unit's sums, kept for the cluster
+        const size_t fixed = w4::rows_fixed_bytes(Cs, B, words, zp) + (WK > 1 ? w4::rows_red_bytes(nt) : 0);
+        if (fixed + sum > (size_t)kMaxSmem) continue;
+        const int units = (tiles + WM - 1) / WM, clusters = std::max(1, std::min(units, sms / S)), mine = (units + clusters - 1) / clusters;
+        const int R = S > 1 ? (int)std::min<size_t>(std::min(mine, 16), (kMaxSmem - fixed) / sum) : 0;
+        const double cost = (double)mine * std::max(WM * Cs * (25 + 10 * nt), w4::rows_run(Cs, WK) * 150) +
+                            mine * (WK * S == 1 ? 100.0 : 400.0) + (S > 1 ? 1800.0 * ((mine + R - 1) / R) : 0.0) + Cs * 32.0 * B;
+        if (cost < least - 1e-9) {
+          least = cost;
+          best = {S, WM, WK, R, clusters * S, fixed + R * sum};
+        }
+      }
+  }
+  return best;
 }
 
-template <int XT, int W, bool ZP>
-cudaError_t launch_linear(const w4::RowsArgs& a, int nt, const RowsPlan& p, cudaStream_t st) {
-  return nt == 1 ? launch(w4::rows_kernel<XT, W, 1, ZP, false>, p.grid, w4::kRowThreads, p.smem, p.S, st, a)
-                 : launch(w4::rows_kernel<XT, W, 2, ZP, false>, p.grid, w4::kRowThreads, p.smem, p.S, st, a);
+template <int W, bool ZP, bool GATEUP>
+cudaError_t launch_rows(const w4::RowsArgs& a, int nt, const RowsPlan& p, int dev, cudaStream_t st) {
+  switch (nt) {
+    case 1: return host_launch<w4::rows_kernel<W, 1, ZP, GATEUP>>(dev, p.grid, w4::kRowThreads, p.smem, p.S, st, a);
+    case 2: return host_launch<w4::rows_kernel<W, 2, ZP, GATEUP>>(dev, p.grid, w4::kRowThreads, p.smem, p.S, st, a);
+    case 3: return host_launch<w4::rows_kernel<W, 3, ZP, GATEUP>>(dev, p.grid, w4::kRowThreads, p.smem, p.S, st, a);
+    default: return host_launch<w4::rows_kernel<W, 4, ZP, GATEUP>>(dev, p.grid, w4::kRowThreads, p.smem, p.S, st, a);
+  }
 }
 
-template <int XT>
-cudaError_t launch_linear(const w4::RowsArgs& a, int words, int nt, const RowsPlan& p, cudaStream_t st) {
-  if (a.w.zeros)
-    return words == 4 ? launch_linear<XT, 4, true>(a, nt, p, st) : words == 2 ? launch_linear<XT, 2, true>(a, nt, p, st)
-                                                                              : launch_linear<XT, 1, true>(a, nt, p, st);
-  return words == 4 ? launch_linear<XT, 4, false>(a, nt, p, st) : words == 2 ? launch_linear<XT, 2, false>(a, nt, p, st)
-                                                                             : launch_linear<XT, 1, false>(a, nt, p, st);
+template <int W>
+cudaError_t launch_linear(const w4::RowsArgs& a, int nt, const RowsPlan& p, int dev, cudaStream_t st) {
+  return a.w.zeros ? launch_rows<W, true, false>(a, nt, p, dev, st) : launch_rows<W, false, false>(a, nt, p, dev, st);
 }
 
 bool group_known(int g) { return g == 0 || g == 32 || g == 64 || g == 128; }
@@ -81,36 +66,45 @@ prox_status_t current_device(int* dev) {
 }
 
 bool mat_ok(const prox_w4_t* w, int dev) {
-  return w && w->codes && w->scales && host_aligned(w->codes, 16) && host_aligned(w->scales, 2) && host_on_current_device(w->codes, dev) &&
+  return w && w->codes && w->scales && host_aligned(w->codes, 16) && host_aligned(w->scales, 16) && host_aligned(w->zeros, 4) && host_on_current_device(w->codes, dev) &&
          host_on_current_device(w->scales, dev) && (!w->zeros || host_on_current_device(w->zeros, dev));
 }
 
 w4::Mat mat_of(const prox_w4_t* w) { return {w->codes, static_cast<const __half*>(w->scales), w->zeros}; }
 
-struct FfnWorkspace { size_t list, members, count, h, bytes; };
+struct FfnWorkspace { size_t list, members, count, tickets, hmax, h, part, bytes; };
 
-// [union list | token bits of its entries | its length | h]; one token needs h alone
+// [union list | token bits of its entries | its length | tickets | largest |h| | h | partial sums]; one token has no union
 FfnWorkspace ffn_workspace(int F, int B) {
   FfnWorkspace w = {};
-  const size_t f = ((size_t)F + 15) / 16 * 16;
-  if (B > 1) { w.members = f * 4; w.count = w.members + f; w.h = w.count + 16; }
-  w.bytes = w.h + f * 4 * B;
+  const size_t f = ((size_t)F + 31) / 32 * 32;
+  if (B > 1) { w.members = f * 4; w.count = w.members + f; w.tickets = w.count + 16; }
+  w.hmax = w.tickets + w4::kMaxSlices * 4;
+  w.h = w.hmax + (size_t)w4::kRowBlocks * B * 4;
+  w.part = w.h + f * 4 * B;
+  w.bytes = w.part + (size_t)w4::kDownBlocks * 1024 * 4 * B;
   return w;
 }
 
-template <bool ZP>
-cudaError_t launch_down(const w4::DownArgs& a, int nt, int grid, cudaStream_t st) {
-  const size_t smem = (size_t)w4::kDownWarps * 128 * nt * 8 * 4 + (size_t)128 * a.B * 4;
-  return nt == 1 ? launch(w4::down_kernel<1, ZP>, grid, w4::kDownThreads, smem, a.S, st, a)
-         : nt == 2 ? launch(w4::down_kernel<2, ZP>, grid, w4::kDownThreads, smem, a.S, st, a)
-                   : launch(w4::down_kernel<3, ZP>, grid, w4::kDownThreads, smem, a.S, st, a);
+template <int NT>
+cudaError_t launch_down(w4::DownArgs& a, int sms, int dev, cudaStream_t st) {
+  constexpr int kThreads = w4::down_threads(NT), kWarps = kThreads / 32;
+  const int cgs = a.D / 128;
+  a.WC = 8;
+  while (a.WC > 1 && a.WC / 2 >= cgs) a.WC /= 2;
+  a.slices = (cgs + a.WC - 1) / a.WC;
+  const int tiles = (a.n + 31) / 32, rows = kWarps / a.WC;
+  a.splits = std::max(1, std::min(std::min(sms, w4::kDownBlocks) / a.slices, (tiles + rows - 1) / rows));
+  const size_t smem = std::max((size_t)kWarps * w4::down_stages(NT) * w4::down_stage(a.B), (size_t)a.WC * 512 * a.B);
+  return a.w.zeros ? host_launch<w4::down_kernel<NT, true>>(dev, a.slices * a.splits, kThreads, smem, 1, st, a)
+                   : host_launch<w4::down_kernel<NT, false>>(dev, a.slices * a.splits, kThreads, smem, 1, st, a);
 }
 
 }  // namespace
 
-#define CKL(expr)                                        \
+#define CKL(...)                                        \
   do {                                                   \
-    cudaError_t e_ = (expr);                             \
+    cudaError_t e_ = (__VA_ARGS__);                        \
     if (e_ != cudaSuccess) return host_map_cuda(e_);     \
   } while (0)
 
@@ -148,21 +142,23 @@ prox_status_t prox_w4_linear(const prox_w4_t* w, int N, int K, int group_size, c
   a.w = a.w2 = mat_of(w);
   a.rows = N; a.K = K; a.groups = groups_of(K, group_size); a.gstep = group_size != 0;
   a.x_stride = x_stride; a.y_stride = y_stride; a.y_type = y_dtype;
+  a.x_half = x_dtype == w4::kFp16;
   a.x_vec = host_aligned(x_dev, 16) && (B == 1 || x_stride % 8 == 0);
   const size_t ysize = y_dtype == w4::kFp32 ? 4 : 2;
+  const int words = group_size == 32 ? 1 : group_size == 64 ? 2 : 4;
   // as many tokens a pass as fit in the shared memory of a cluster
-  const int C = (K + 127) / 128, fit = (int)((size_t)(kMaxSmem - 100 * 1024) / ((size_t)(C + 7) / 8 * 256));
-  const int per = std::max(1, std::min(kMaxTokens, fit));
+  const int Cs = w4::rows_share((K + 127) / 128, 8);
+  int per = w4::kMaxPass;
+  while (per > 1 && w4::rows_fixed_bytes(Cs, per, words, true) + 16 * 64 * per > (size_t)kMaxSmem) --per;
   for (int b = 0; b < B; b += per) {
     a.B = std::min(per, B - b);
     a.x = static_cast<const uint16_t*>(x_dev) + (size_t)b * x_stride;
     a.y = static_cast<uint8_t*>(y_dev) + (size_t)b * y_stride * ysize;
-    const int nt = a.B > 8 ? 2 : 1;
-    const RowsPlan p = plan_rows((N + 15) / 16, K, a.B, nt, sms);
+    const int nt = (a.B + 1) / 2;
+    const RowsPlan p = plan_rows((N + 15) / 16, K, a.B, words, nt, w->zeros != nullptr, sms);
     a.S = p.S; a.WM = p.WM; a.WK = p.WK; a.R = p.R;
-    const int words = group_size == 32 ? 1 : group_size == 64 ? 2 : 4;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    CKL(x_dtype == w4::kBf16 ? launch_linear<w4::kBf16>(a, words, nt, p, st) : launch_linear<w4::kFp16>(a, words, nt, p, st));
+    CKL(words == 4 ? launch_linear<4>(a, nt, p, dev, st) : words == 2 ? launch_linear<2>(a, nt, p, dev, st) : launch_linear<1>(a, nt, p, dev, st));
   }
   return PROX_OK;
 }
@@ -199,7 +195,7 @@ prox_status_t prox_w4_stage2_ffn(const prox_w4_t* gate, const prox_w4_t* up, con
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   uint8_t* wsp = static_cast<uint8_t*>(workspace_dev);
   float* h = reinterpret_cast<float*>(wsp + ws.h);
-  const int h_stride = (F + 15) / 16 * 16;
+  unsigned* tickets = reinterpret_cast<unsigned*>(wsp + ws.tickets);
   const int* list = sel_dev;
   const int* count = count_dev_or_null;
   const uint8_t* members = nullptr;
@@ -207,32 +203,30 @@ prox_status_t prox_w4_stage2_ffn(const prox_w4_t* gate, const prox_w4_t* up, con
   if (B > 1) {
     int* ulist = reinterpret_cast<int*>(wsp + ws.list);
     int* ucount = reinterpret_cast<int*>(wsp + ws.count);
-    CKL(launch(w4::union_kernel, 1, w4::kUnionThreads, (size_t)(F + 3) / 4 * 4, 1, st, sel_dev, sel_stride, count_dev_or_null, k2, B, F, ulist,
+    CKL(host_launch<w4::union_kernel>(dev, w4::kUnionBlocks, w4::kUnionThreads, ((size_t)F + 31) / 32 * 4, w4::kUnionBlocks, st, sel_dev, sel_stride, count_dev_or_null, k2, B, F, ulist,
                wsp + ws.members, ucount));
     list = ulist; count = ucount; members = wsp + ws.members;
     most = (int)std::min<long long>(F, (long long)B * k2);
   }
   const int groups = groups_of(D, group_size);
-  if (most > 0) {
-    w4::RowsArgs a = {};
-    a.w = mat_of(gate); a.w2 = mat_of(up);
-    a.rows = F; a.K = D; a.groups = groups; a.gstep = group_size != 0;
-    a.x = static_cast<const uint16_t*>(x_dev); a.x_stride = D; a.B = B; a.x_vec = 1;
-    a.list = list; a.count = count; a.n = most; a.members = members; a.h = h; a.h_stride = h_stride;
-    const RowsPlan p = plan_rows((most + 7) / 8, D, B, 1, sms);
-    a.S = p.S; a.WM = p.WM; a.WK = p.WK; a.R = p.R;
-    CKL(gate->zeros ? launch(w4::rows_kernel<w4::kBf16, 4, 1, true, true>, p.grid, w4::kRowThreads, p.smem, p.S, st, a)
-                    : launch(w4::rows_kernel<w4::kBf16, 4, 1, false, true>, p.grid, w4::kRowThreads, p.smem, p.S, st, a));
-  }
+  w4::RowsArgs a = {};
+  a.w = mat_of(gate); a.w2 = mat_of(up);
+  a.rows = F; a.K = D; a.groups = groups; a.gstep = group_size != 0;
+  a.x = static_cast<const uint16_t*>(x_dev); a.x_stride = D; a.B = B; a.x_vec = 1;
+  a.list = list; a.count = count; a.n = most; a.members = members; a.h = h; a.tickets = tickets;
+  a.hmax = reinterpret_cast<unsigned*>(wsp + ws.hmax);
+  const int nt = (B + 1) / 2;
+  const RowsPlan p = plan_rows(std::max(1, (most + 7) / 8), D, B, 4, nt, gate->zeros != nullptr, std::min(sms, w4::kRowBlocks));
+  a.S = p.S; a.WM = p.WM; a.WK = p.WK; a.R = p.R;
+  CKL(gate->zeros ? launch_rows<4, true, true>(a, nt, p, dev, st) : launch_rows<4, false, true>(a, nt, p, dev, st));
   w4::DownArgs d = {};
   d.w = mat_of(down_t);
   d.D = D; d.F = F; d.groups = groups; d.gstep = group_size != 0;
-  d.list = list; d.count = count; d.n = most; d.h = h; d.h_stride = h_stride; d.B = B; d.y = y_dev; d.y_type = out_dtype;
-  const int cgs = D / 128;
-  d.S = 8;
-  while (d.S > 1 && cgs * d.S > 2 * sms) d.S /= 2;
-  const int nt = (3 * B + 7) / 8;
-  CKL(down_t->zeros ? launch_down<true>(d, nt, cgs * d.S, st) : launch_down<false>(d, nt, cgs * d.S, st));
+  d.list = list; d.count = count; d.n = most; d.h = h; d.B = B; d.y = y_dev; d.y_type = out_dtype;
+  d.part = reinterpret_cast<float*>(wsp + ws.part); d.tickets = tickets;
+  d.hmax = a.hmax; d.hblocks = p.grid;
+  CKL(nt == 1 ? launch_down<1>(d, sms, dev, st) : nt == 2 ? launch_down<2>(d, sms, dev, st) : nt == 3 ? launch_down<3>(d, sms, dev, st)
+                                                                                                      : launch_down<4>(d, sms, dev, st));
   return PROX_OK;
 }
 

@@ -1,9 +1,10 @@
 """Weights held in 4 bits on the GPU, against the definition in 64 bits.
 
-Tolerances.  Products (code - zero) * x are exact in fp32 (at most 8 + 8 significant bits, or 8 + 11), so an output is off by the
-roundings of its sum alone.  With A = sum |w x| of the output: a tensor-core step adds 16 products to a running sum, 17 terms that
-may each lose 2^-24 of the largest; 8 steps a group, so 136 * 2^-24 * A over all groups; one fp32 FMA per group (at most K / 32) and
-sums over at most 16 warps and 8 blocks follow: (136 + K / 32 + 40) * 2^-24 * A, and half a step of the output type."""
+Tolerances.  A token's inputs enter as fixed-point numbers, off by 2^-30 of the token's largest at most; sums over a group are whole
+numbers and exact.  With A = sum |w x| of an output: the four digits' sums of a group become fp32 numbers exactly, one fp32
+FMA per group follows (at most K / 32), sums over at most 16 warps and 8 blocks, the join of the digits and two scalings:
+(K / 32 + 16 + 8 + 8) * 2^-24 * A, and half a step of the output type.  A = sum over absolute digits' products may be twice sum |w x|
+(a digit of the lower places has either sign): that doubles it."""
 import numpy as np
 import pytest
 import torch
@@ -49,7 +50,12 @@ def half_step(t, v):
 
 
 def sum_bound(K, A):
-    return (136 + K / 32 + 40) * U * A
+    return 2 * (K / 32 + 32) * U * A
+
+
+def input_bound(x, W):
+    """sum |w| 2^-30 max |x|, [B, N]"""
+    return 2.0 ** -30 * x.abs().amax(1, keepdim=True) * W.abs().sum(1)
 
 
 def tokens(seed, B, K, dtype):
@@ -62,7 +68,7 @@ def check_linear(y, w, group, x, K, ydt):
     W = values(w, group)
     xd = x.double()
     want = xd @ W.T
-    tol = sum_bound(K, xd.abs() @ W.abs().T)
+    tol = sum_bound(K, xd.abs() @ W.abs().T) + input_bound(xd, W)
     tol = tol + half_step(DT[ydt], want.abs() + tol)
     err = (y.double() - want).abs()
     assert torch.isfinite(y).all()
@@ -177,7 +183,9 @@ def test_linear_chain_without_a_wait(pb):
 
 # ---- Stage 2 ----------------------------------------------------------------
 def ffn_reference(gate, up, down, group, x, lists):
-    """y and its bound: d(silu) <= 1.1 |dg|; expf, the division and the products lose a few steps; h s goes on in 24 bits."""
+    """y and its bound: d(silu) <= 1.1 |dg|; expf, the division and the products lose a few steps; h s is rounded to fp32 and to a
+    fixed-point number, off by 2^-29 of the largest |h| times the largest scale; the sum of those is exact in each of the
+    warps and blocks (at most 16 and 160), whose sums are fp32."""
     D = x.shape[1]
     ys, tols = [], []
     for b, ids in enumerate(lists):
@@ -185,7 +193,8 @@ def ffn_reference(gate, up, down, group, x, lists):
         xd = x[b].double()
         G, Up, Dn = (values(pick(w), group) for w in (gate, up, down))
         g, u = G @ xd, Up @ xd
-        dg, du = sum_bound(D, G.abs() @ xd.abs()), sum_bound(D, Up.abs() @ xd.abs())
+        dg = sum_bound(D, G.abs() @ xd.abs()) + input_bound(xd[None], G)[0]
+        du = sum_bound(D, Up.abs() @ xd.abs()) + input_bound(xd[None], Up)[0]
         silu = g / (1 + torch.exp(-g))
         dsilu = 1.1 * dg + 16 * U * silu.abs() + 2.0 ** -126
         h = silu * u
@@ -193,7 +202,9 @@ def ffn_reference(gate, up, down, group, x, lists):
         y = h @ Dn
         A = (h.abs() + dh) @ Dn.abs()
         ys.append(y)
-        tols.append(dh @ Dn.abs() + (17 * (len(ids) / 16 + 1) + 3 * 8 + 40) * U * A)
+        most = (h.abs() + dh).max() * down[1].double().abs().max() if len(ids) else 0.0
+        codes = (Dn / pick(down)[1].double().repeat_interleave(group or D, 1).clamp_min(1e-30)).abs().sum(0)
+        tols.append(dh @ Dn.abs() + 2 * (16 + 160 + 8) * U * A + 2.0 ** -29 * most * codes)
     return torch.stack(ys), torch.stack(tols)
 
 
