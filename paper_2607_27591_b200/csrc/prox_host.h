@@ -38,17 +38,21 @@ inline int host_sm_count(int device) {
 
 constexpr int kMaxBlockSmem = 227 * 1024;
 
+// Lets a kernel have all the shared memory of an SM (once per device).
+template <auto Kern>
+cudaError_t host_allow_smem(int device) {
+  static bool allowed[64] = {};
+  if (allowed[device & 63]) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(Kern), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxBlockSmem - 4096);
+  if (e == cudaSuccess) allowed[device & 63] = true;
+  return e;
+}
+
 // A launch that may be set up while its predecessor on the stream still runs (the kernel waits for it before it reads
 // anything), of clusters of `cluster` blocks.
 template <auto Kern, typename... Args>
 cudaError_t host_launch(int device, unsigned grid, int block, size_t smem, int cluster, cudaStream_t st, Args... args) {
-  static bool allowed[64] = {};                    // per device: more dynamic shared memory than the default has been asked for
-  if (!allowed[device & 63]) {
-    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(Kern), cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               kMaxBlockSmem - 1024);
-    if (e != cudaSuccess) return e;
-    allowed[device & 63] = true;
-  }
+  if (const cudaError_t e = host_allow_smem<Kern>(device)) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid); cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cudaLaunchAttribute at[2];

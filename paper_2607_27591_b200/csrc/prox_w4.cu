@@ -8,28 +8,48 @@ using namespace prox;
 
 namespace {
 
-constexpr int kMaxSmem = kMaxBlockSmem - 1024;   // dynamic; the kernels have a few words of their own
+constexpr int kMaxSmem = kMaxBlockSmem - 4096;   // dynamic; the kernels have up to 4 KB of their own
 constexpr int kFfnTokens = 8;            // tokens of a call of the sparse FFN, as everywhere in the library
 
 // Shape of a launch of rows_kernel for `tiles` tiles of 16 rows.
 struct RowsPlan { int S, WM, WK, R, grid; size_t smem; };
 
+// Clusters of S blocks that the GPU holds at once (a block of these kernels has an SM to itself).
+template <auto Kern>
+int clusters_at_once(int device, int S, int threads, size_t smem) {
+  static int known[64][9] = {};
+  int& n = known[device & 63][S];
+  if (n > 0) return n;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(S); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = S; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  cfg.attrs = at; cfg.numAttrs = 1;
+  if (host_allow_smem<Kern>(device) != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, Kern, &cfg) != cudaSuccess || n < 1) {
+    (void)cudaGetLastError();
+    n = std::max(1, 128 / S);
+  }
+  return n;
+}
+
 // The shape that is done first, in cycles: an SM takes about 35 for 128 columns of a tile when all its warps are busy (10
 // more for every 8 columns of digits), a warp alone 150; the end of a unit costs 400, less where no warp waits for another, the
 // cluster's sum 1800; a token's digits are made at 4 inputs a cycle.
-RowsPlan plan_rows(int tiles, int K, int B, int words, int nt, bool zp, int sms) {
+RowsPlan plan_rows(int tiles, int K, int B, int words, int nt, bool zp, int sms, int dev) {
   const int C = (K + 127) / 128;
   RowsPlan best = {};
   double least = 1e30;
   for (int S = 1; S <= 8; S *= 2) {
     const int Cs = w4::rows_share(C, S);
+    const int at_once = S == 1 ? sms : std::min(sms / S, clusters_at_once<w4::rows_kernel<4, 1, false, false>>(dev, S, w4::kRowThreads, 120 * 1024));
     if (S > 1 && Cs * (S - 1) >= C) break;                   // a block without columns
     for (int WK = 1; WK <= w4::kRowWarps && WK <= 2 * Cs - 1; WK *= 2)
       for (int WM = w4::kRowWarps / WK; WM >= 1; WM /= 2) {
         const size_t sum = S > 1 ? (size_t)WM * 64 * B : 0;  // a unit's sums, kept for the cluster
-        const size_t fixed = w4::rows_fixed_bytes(Cs, B, words, zp) + (WK > 1 ? w4::rows_red_bytes(nt) : 0);
+        const size_t fixed = w4::rows_fixed_bytes(Cs, nt, words, zp) + (WK > 1 ? w4::rows_red_bytes(nt) : 0);
         if (fixed + sum > (size_t)kMaxSmem) continue;
-        const int units = (tiles + WM - 1) / WM, clusters = std::max(1, std::min(units, sms / S)), mine = (units + clusters - 1) / clusters;
+        const int units = (tiles + WM - 1) / WM, clusters = std::max(1, std::min(units, at_once)), mine = (units + clusters - 1) / clusters;
         const int R = S > 1 ? (int)std::min<size_t>(std::min(mine, 16), (kMaxSmem - fixed) / sum) : 0;
         const double cost = (double)mine * std::max(WM * Cs * (25 + 10 * nt), w4::rows_run(Cs, WK) * 150) +
                             mine * (WK * S == 1 ? 100.0 : 400.0) + (S > 1 ? 1800.0 * ((mine + R - 1) / R) : 0.0) + Cs * 32.0 * B;
@@ -66,38 +86,46 @@ prox_status_t current_device(int* dev) {
 }
 
 bool mat_ok(const prox_w4_t* w, int dev) {
-  return w && w->codes && w->scales && host_aligned(w->codes, 16) && host_aligned(w->scales, 16) && host_aligned(w->zeros, 4) && host_on_current_device(w->codes, dev) &&
+  return w && w->codes && w->scales && host_aligned(w->codes, 16) && host_aligned(w->scales, 16) && host_aligned(w->zeros, 16) && host_on_current_device(w->codes, dev) &&
          host_on_current_device(w->scales, dev) && (!w->zeros || host_on_current_device(w->zeros, dev));
 }
 
 w4::Mat mat_of(const prox_w4_t* w) { return {w->codes, static_cast<const __half*>(w->scales), w->zeros}; }
 
-struct FfnWorkspace { size_t list, members, count, tickets, hmax, h, part, bytes; };
+struct FfnWorkspace { size_t list, members, count, hmax, h, bytes; };
 
-// [union list | token bits of its entries | its length | tickets | largest |h| | h | partial sums]; one token has no union
+// [union list | token bits of its entries | its length | largest |h| | h]; one token has no union
 FfnWorkspace ffn_workspace(int F, int B) {
   FfnWorkspace w = {};
   const size_t f = ((size_t)F + 31) / 32 * 32;
-  if (B > 1) { w.members = f * 4; w.count = w.members + f; w.tickets = w.count + 16; }
-  w.hmax = w.tickets + w4::kMaxSlices * 4;
+  if (B > 1) { w.members = f * 4; w.count = w.members + f; w.hmax = w.count + 16; }
   w.h = w.hmax + (size_t)w4::kRowBlocks * B * 4;
-  w.part = w.h + f * 4 * B;
-  w.bytes = w.part + (size_t)w4::kDownBlocks * 1024 * 4 * B;
+  w.bytes = w.h + f * 4 * B;
   return w;
 }
 
-template <int NT>
-cudaError_t launch_down(w4::DownArgs& a, int sms, int dev, cudaStream_t st) {
+template <int NT, bool ZP>
+cudaError_t launch_down(w4::DownArgs& a, int dev, cudaStream_t st) {
   constexpr int kThreads = w4::down_threads(NT), kWarps = kThreads / 32;
-  const int cgs = a.D / 128;
-  a.WC = 8;
-  while (a.WC > 1 && a.WC / 2 >= cgs) a.WC /= 2;
-  a.slices = (cgs + a.WC - 1) / a.WC;
-  const int tiles = (a.n + 31) / 32, rows = kWarps / a.WC;
-  a.splits = std::max(1, std::min(std::min(sms, w4::kDownBlocks) / a.slices, (tiles + rows - 1) / rows));
-  const size_t smem = std::max((size_t)kWarps * w4::down_stages(NT) * w4::down_stage(a.B), (size_t)a.WC * 512 * a.B);
-  return a.w.zeros ? host_launch<w4::down_kernel<NT, true>>(dev, a.slices * a.splits, kThreads, smem, 1, st, a)
-                   : host_launch<w4::down_kernel<NT, false>>(dev, a.slices * a.splits, kThreads, smem, 1, st, a);
+  constexpr auto kern = w4::down_kernel<NT, ZP>;
+  const int cgs = a.D / 128, tiles = std::max(1, (a.n + 31) / 32);
+  const size_t smem = std::max((size_t)kWarps * w4::down_stages(NT) * w4::down_stage(a.B), (size_t)kWarps * 512 * a.B);
+  // the shape with the fewest rounds of a tile for every warp; a cluster's sum counts as one
+  double least = 1e30;
+  for (int S = 8; S >= 1; S /= 2)
+    for (int WC = 8; WC >= 1; WC /= 2) {
+      const int slices = (cgs + WC - 1) / WC, at_once = S == 1 ? 148 : clusters_at_once<kern>(dev, S, kThreads, smem);
+      const int waves = (slices + at_once - 1) / at_once, rounds = ((tiles + S - 1) / S + kWarps / WC - 1) / (kWarps / WC);
+      if (tiles > 1024 * S) continue;                          // (32768 entries a block: its sums stay below 2^31)
+      const double cost = waves * (rounds + 2.0) + (S > 1 ? 1.0 : 0.0) - 0.01 * WC;
+      if (cost < least) { least = cost; a.S = S; a.WC = WC; }
+    }
+  return host_launch<kern>(dev, (cgs + a.WC - 1) / a.WC * a.S, kThreads, smem, a.S, st, a);
+}
+
+template <int NT>
+cudaError_t launch_down(w4::DownArgs& a, int dev, cudaStream_t st) {
+  return a.w.zeros ? launch_down<NT, true>(a, dev, st) : launch_down<NT, false>(a, dev, st);
 }
 
 }  // namespace
@@ -149,13 +177,13 @@ prox_status_t prox_w4_linear(const prox_w4_t* w, int N, int K, int group_size, c
   // as many tokens a pass as fit in the shared memory of a cluster
   const int Cs = w4::rows_share((K + 127) / 128, 8);
   int per = w4::kMaxPass;
-  while (per > 1 && w4::rows_fixed_bytes(Cs, per, words, true) + 16 * 64 * per > (size_t)kMaxSmem) --per;
+  while (per > 1 && w4::rows_fixed_bytes(Cs, (per + 1) / 2, words, w->zeros != nullptr) + 16 * 64 * per > (size_t)kMaxSmem) --per;
   for (int b = 0; b < B; b += per) {
     a.B = std::min(per, B - b);
     a.x = static_cast<const uint16_t*>(x_dev) + (size_t)b * x_stride;
     a.y = static_cast<uint8_t*>(y_dev) + (size_t)b * y_stride * ysize;
     const int nt = (a.B + 1) / 2;
-    const RowsPlan p = plan_rows((N + 15) / 16, K, a.B, words, nt, w->zeros != nullptr, sms);
+    const RowsPlan p = plan_rows((N + 15) / 16, K, a.B, words, nt, w->zeros != nullptr, sms, dev);
     a.S = p.S; a.WM = p.WM; a.WK = p.WK; a.R = p.R;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     CKL(words == 4 ? launch_linear<4>(a, nt, p, dev, st) : words == 2 ? launch_linear<2>(a, nt, p, dev, st) : launch_linear<1>(a, nt, p, dev, st));
@@ -195,7 +223,6 @@ prox_status_t prox_w4_stage2_ffn(const prox_w4_t* gate, const prox_w4_t* up, con
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   uint8_t* wsp = static_cast<uint8_t*>(workspace_dev);
   float* h = reinterpret_cast<float*>(wsp + ws.h);
-  unsigned* tickets = reinterpret_cast<unsigned*>(wsp + ws.tickets);
   const int* list = sel_dev;
   const int* count = count_dev_or_null;
   const uint8_t* members = nullptr;
@@ -213,20 +240,19 @@ prox_status_t prox_w4_stage2_ffn(const prox_w4_t* gate, const prox_w4_t* up, con
   a.w = mat_of(gate); a.w2 = mat_of(up);
   a.rows = F; a.K = D; a.groups = groups; a.gstep = group_size != 0;
   a.x = static_cast<const uint16_t*>(x_dev); a.x_stride = D; a.B = B; a.x_vec = 1;
-  a.list = list; a.count = count; a.n = most; a.members = members; a.h = h; a.tickets = tickets;
+  a.list = list; a.count = count; a.n = most; a.members = members; a.h = h;
   a.hmax = reinterpret_cast<unsigned*>(wsp + ws.hmax);
   const int nt = (B + 1) / 2;
-  const RowsPlan p = plan_rows(std::max(1, (most + 7) / 8), D, B, 4, nt, gate->zeros != nullptr, std::min(sms, w4::kRowBlocks));
+  const RowsPlan p = plan_rows(std::max(1, (most + 7) / 8), D, B, 4, nt, gate->zeros != nullptr, std::min(sms, w4::kRowBlocks), dev);
   a.S = p.S; a.WM = p.WM; a.WK = p.WK; a.R = p.R;
   CKL(gate->zeros ? launch_rows<4, true, true>(a, nt, p, dev, st) : launch_rows<4, false, true>(a, nt, p, dev, st));
   w4::DownArgs d = {};
   d.w = mat_of(down_t);
   d.D = D; d.F = F; d.groups = groups; d.gstep = group_size != 0;
   d.list = list; d.count = count; d.n = most; d.h = h; d.B = B; d.y = y_dev; d.y_type = out_dtype;
-  d.part = reinterpret_cast<float*>(wsp + ws.part); d.tickets = tickets;
   d.hmax = a.hmax; d.hblocks = p.grid;
-  CKL(nt == 1 ? launch_down<1>(d, sms, dev, st) : nt == 2 ? launch_down<2>(d, sms, dev, st) : nt == 3 ? launch_down<3>(d, sms, dev, st)
-                                                                                                      : launch_down<4>(d, sms, dev, st));
+  CKL(nt == 1 ? launch_down<1>(d, dev, st) : nt == 2 ? launch_down<2>(d, dev, st) : nt == 3 ? launch_down<3>(d, dev, st)
+                                                                                                      : launch_down<4>(d, dev, st));
   return PROX_OK;
 }
 
