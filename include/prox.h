@@ -399,6 +399,24 @@ prox_status_t prox_w4_stage2_ffn(const prox_w4_t* gate, const prox_w4_t* up, con
                                  int sel_stride, const int32_t* count_dev_or_null, int k2, void* y_dev, int out_dtype,
                                  void* workspace_dev, int64_t workspace_bytes, void* stream);
 
+/* ---- Log probabilities from logits: what a decode step is asked for beside its token, and what perplexity and the
+ * scoring of choices are made of (the paper's evaluation).  With z = x / temperature and p = softmax(z) of a row:
+ *   logits      dev bf16, fp32 or fp16 (dtype 0, 1, 2) [T, V], rows row_stride elements apart (any alignment of the type's size)
+ *   temperature 1e-30 .. 1e30
+ *   given       dev int32 [T, n_given] (NULL if n_given = 0): token ids
+ *   logprob     dev fp32 [T, n_given]: log p of them; 0 for a negative id (no token), NaN for one from V on
+ *   entropy     dev fp32 [T] or NULL: -sum p log p, in nats
+ *   n_top       0..32, at most V: the likeliest tokens, by logit, equal ones by the lower id
+ *   top_logprob, top_index   dev fp32 / int32 [T, n_top] (NULL if n_top = 0), likeliest first
+ * A logit of -inf has log p = -inf.  A row of nothing but -inf has log p = -inf everywhere and entropy 0.  A row with a NaN or
+ * +inf has NaN in all its log probabilities and its entropy; a NaN comes first among its top tokens.
+ * The logits are read once; results are the same on every call.  Every buffer has to lie on the current device.
+ * Errors: INVALID_ARG, UNSUPPORTED (n_top > 32, V near 2^31), CUDA. */
+prox_status_t prox_token_logprobs(const void* logits_dev, int dtype, int T, int V, int64_t row_stride,
+                                  float temperature, const int32_t* given_dev, int n_given, float* logprob_dev,
+                                  float* entropy_dev_or_null, int n_top, float* top_logprob_dev,
+                                  int32_t* top_index_dev, void* stream);
+
 /* Runtime mask counts accumulated by the threshold entry points since the last
  * reset (appendix "Threshold Calibration and Runtime Sparsity":
  * e^ = s2^ - 2 alpha (1 - s1^) / 3).  Host-synchronous.  Any pointer may be NULL. */

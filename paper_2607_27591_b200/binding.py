@@ -92,6 +92,7 @@ _SIGS = {
     "prox_w4_stage2_workspace": [_i, _i, _i, C.POINTER(C.c_int64)],
     "prox_w4_stage2_ffn": [C.POINTER(ProxW4), C.POINTER(ProxW4), C.POINTER(ProxW4), _i, _i, _i, _vp, _i, _vp, _i, _vp, _i, _vp, _i,
                            _vp, C.c_int64, _vp],
+    "prox_token_logprobs": [_vp, _i, _i, _i, C.c_int64, _f, _vp, _i, _vp, _vp, _i, _vp, _vp, _vp],
     "prox_profile_enable": [_vp, _i],
     "prox_profile_read": [_vp, C.POINTER(C.c_int64), C.POINTER(_d)],
 }
@@ -329,6 +330,13 @@ def prox_w4_stage2_ffn(gate, up, down_t, d_model: int, d_ff: int, group_size: in
     _check(_lib.prox_w4_stage2_ffn(C.byref(_w4(gate)), C.byref(_w4(up)), C.byref(_w4(down_t)), d_model, d_ff, group_size, _ptr(x), B, _ptr(sel),
                                    sel_stride, _ptr(count), k2, _ptr(y), out_dtype, _ptr(workspace), workspace_bytes, _ptr(stream)),
            "prox_w4_stage2_ffn")
+
+
+def prox_token_logprobs(logits, dtype: int, T: int, V: int, row_stride: int, temperature: float, given, n_given: int, logprob, entropy,
+                        n_top: int, top_logprob, top_index, stream=None) -> None:
+    """given, logprob may be None with n_given = 0; entropy may be None; top_logprob, top_index may be None with n_top = 0."""
+    _check(_lib.prox_token_logprobs(_ptr(logits), dtype, T, V, row_stride, temperature, _ptr(given), n_given, _ptr(logprob), _ptr(entropy),
+                                    n_top, _ptr(top_logprob), _ptr(top_index), _ptr(stream)), "prox_token_logprobs")
 
 
 def prox_calibrate_stack(handles, d_ff: int, norm_w, eps: float, x_res_tokens, s1: float, s2: float,

@@ -38,7 +38,7 @@ inline int host_sm_count(int device) {
 
 constexpr int kMaxBlockSmem = 227 * 1024;
 
-// Lets a kernel have all the shared memory of an SM (once per device).
+// Lets a kernel with dynamic shared memory have that of a whole SM (once per device).
 template <auto Kern>
 cudaError_t host_allow_smem(int device) {
   static bool allowed[64] = {};
@@ -52,7 +52,9 @@ cudaError_t host_allow_smem(int device) {
 // anything), of clusters of `cluster` blocks.
 template <auto Kern, typename... Args>
 cudaError_t host_launch(int device, unsigned grid, int block, size_t smem, int cluster, cudaStream_t st, Args... args) {
-  if (const cudaError_t e = host_allow_smem<Kern>(device)) return e;
+  if (smem > 0) {
+    if (const cudaError_t e = host_allow_smem<Kern>(device)) return e;
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid); cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cudaLaunchAttribute at[2];
