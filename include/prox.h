@@ -351,7 +351,7 @@ prox_status_t prox_rmsnorm(prox_ffn_t* h, const float* x_res_dev, const void* no
  *   codes   dev uint8 [rows, cols / 2], 16-byte aligned: byte i holds column 2i in bits 0-3, column 2i + 1 in bits 4-7
  *   scales  dev fp16 [rows, groups], groups = ceil(cols / G) (the last group may be shorter), 16-byte aligned
  *   zeros   dev uint8 [rows, groups] of 0..16, 16-byte aligned, or NULL: 8 everywhere (symmetric codes)
- * All three are read in place.  A token's inputs enter as fixed-point numbers of 30 bits below its largest, sums over a
+ * All three are read in place.  A token's inputs enter as fixed-point numbers of 26 bits below its largest, sums over a
  * group are exact, sums of groups fp32; results are the same on every call.  A token with an input that is not finite
  * gets NaN.  Data types are numbered 0 = bf16, 1 = fp32, 2 = fp16.
  * Every buffer has to lie on the current device (or in pinned mapped or managed memory); others are refused. */

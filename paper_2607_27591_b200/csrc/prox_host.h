@@ -43,7 +43,7 @@ template <auto Kern>
 cudaError_t host_allow_smem(int device) {
   static bool allowed[64] = {};
   if (allowed[device & 63]) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(Kern), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxBlockSmem - 4096);
+  const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(Kern), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxBlockSmem - 8192);
   if (e == cudaSuccess) allowed[device & 63] = true;
   return e;
 }

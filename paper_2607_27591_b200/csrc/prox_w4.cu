@@ -8,11 +8,12 @@ using namespace prox;
 
 namespace {
 
-constexpr int kMaxSmem = kMaxBlockSmem - 4096;   // dynamic; the kernels have up to 4 KB of their own
+constexpr int kMaxSmem = kMaxBlockSmem - 8192;   // dynamic; the kernels have up to 8 KB of their own
+constexpr int kMaxRowBlocks = 256;       // of the gate and up kernel
 constexpr int kFfnTokens = 8;            // tokens of a call of the sparse FFN, as everywhere in the library
 
 // Shape of a launch of rows_kernel for `tiles` tiles of 16 rows.
-struct RowsPlan { int S, WM, WK, R, grid; size_t smem; };
+struct RowsPlan { int S, WM, WK, stages, R, grid; size_t smem; };
 
 // Clusters of S blocks that the GPU holds at once (a block of these kernels has an SM to itself).
 template <auto Kern>
@@ -33,10 +34,10 @@ int clusters_at_once(int device, int S, int threads, size_t smem) {
   return n;
 }
 
-// The shape that is done first, in cycles: an SM takes about 35 for 128 columns of a tile when all its warps are busy (10
-// more for every 8 columns of digits), a warp alone 150; the end of a unit costs 400, less where no warp waits for another, the
-// cluster's sum 1800; a token's digits are made at 4 inputs a cycle.
-RowsPlan plan_rows(int tiles, int K, int B, int words, int nt, bool zp, int sms, int dev) {
+// The shape that is done first, in cycles: an SM takes about 48 for 128 columns of a tile when all its warps are busy (18
+// more for every 8 further columns of digits), a warp alone 300 (100 more); the end of a unit costs 1500, much less where no warp waits for
+// another, the cluster's sum 5000; a token's digits are made at 4 inputs a cycle.
+RowsPlan plan_rows(int tiles, int K, int B, int words, int nt, int sms, int dev) {
   const int C = (K + 127) / 128;
   RowsPlan best = {};
   double least = 1e30;
@@ -45,19 +46,22 @@ RowsPlan plan_rows(int tiles, int K, int B, int words, int nt, bool zp, int sms,
     const int at_once = S == 1 ? sms : std::min(sms / S, clusters_at_once<w4::rows_kernel<4, 1, false, false>>(dev, S, w4::kRowThreads, 120 * 1024));
     if (S > 1 && Cs * (S - 1) >= C) break;                   // a block without columns
     for (int WK = 1; WK <= w4::kRowWarps && WK <= 2 * Cs - 1; WK *= 2)
-      for (int WM = w4::kRowWarps / WK; WM >= 1; WM /= 2) {
-        const size_t sum = S > 1 ? (size_t)WM * 64 * B : 0;  // a unit's sums, kept for the cluster
-        const size_t fixed = w4::rows_fixed_bytes(Cs, nt, words, zp) + (WK > 1 ? w4::rows_red_bytes(nt) : 0);
-        if (fixed + sum > (size_t)kMaxSmem) continue;
-        const int units = (tiles + WM - 1) / WM, clusters = std::max(1, std::min(units, at_once)), mine = (units + clusters - 1) / clusters;
-        const int R = S > 1 ? (int)std::min<size_t>(std::min(mine, 16), (kMaxSmem - fixed) / sum) : 0;
-        const double cost = (double)mine * std::max(WM * Cs * (25 + 10 * nt), w4::rows_run(Cs, WK) * 150) +
-                            mine * (WK * S == 1 ? 100.0 : 400.0) + (S > 1 ? 1800.0 * ((mine + R - 1) / R) : 0.0) + Cs * 32.0 * B;
-        if (cost < least - 1e-9) {
-          least = cost;
-          best = {S, WM, WK, R, clusters * S, fixed + R * sum};
+      for (int WM = w4::kRowWarps / WK; WM >= 1; WM /= 2)
+        for (int stages : {w4::kMaxStages, 3, 2}) {
+          const size_t sum = S > 1 ? (size_t)WM * 64 * B : 0;  // a unit's sums, kept for the cluster
+          const size_t fixed = w4::rows_fixed_bytes(Cs, nt, words) + (WK > 1 ? w4::rows_red_bytes(nt) : 0) +
+                               (size_t)w4::kRowWarps * stages * w4::rows_stage_bytes(words);
+          if (fixed + sum > (size_t)kMaxSmem) continue;
+          const int units = (tiles + WM - 1) / WM, clusters = std::max(1, std::min(units, at_once)), mine = (units + clusters - 1) / clusters;
+          const int R = S > 1 ? (int)std::min<size_t>(std::min(mine, 16), (kMaxSmem - fixed) / sum) : 0;
+          const double cost = (double)mine * std::max(WM * Cs * (30 + 18 * nt), w4::rows_run(Cs, WK) * (200 + 100 * nt)) * (1.0 + 0.3 / stages) +
+                              mine * (WK == 1 ? 300.0 : 1500.0) + (S > 1 ? 5000.0 * ((mine + R - 1) / R) : 0.0) + Cs * 32.0 * B;
+          if (cost < least - 1e-9) {
+            least = cost;
+            best = {S, WM, WK, stages, R, clusters * S, fixed + R * sum};
+          }
+          break;                                               // (the most stages that fit)
         }
-      }
   }
   return best;
 }
@@ -99,7 +103,7 @@ FfnWorkspace ffn_workspace(int F, int B) {
   FfnWorkspace w = {};
   const size_t f = ((size_t)F + 31) / 32 * 32;
   if (B > 1) { w.members = f * 4; w.count = w.members + f; w.hmax = w.count + 16; }
-  w.h = w.hmax + (size_t)w4::kRowBlocks * B * 4;
+  w.h = w.hmax + (size_t)kMaxRowBlocks * B * 4;
   w.bytes = w.h + f * 4 * B;
   return w;
 }
@@ -177,14 +181,14 @@ prox_status_t prox_w4_linear(const prox_w4_t* w, int N, int K, int group_size, c
   // as many tokens a pass as fit in the shared memory of a cluster
   const int Cs = w4::rows_share((K + 127) / 128, 8);
   int per = w4::kMaxPass;
-  while (per > 1 && w4::rows_fixed_bytes(Cs, (per + 1) / 2, words, w->zeros != nullptr) + 16 * 64 * per > (size_t)kMaxSmem) --per;
+  while (per > 1 && w4::rows_fixed_bytes(Cs, (per + 1) / 2, words) + 32 * w4::rows_stage_bytes(words) + 16 * 64 * per > (size_t)kMaxSmem) --per;
   for (int b = 0; b < B; b += per) {
     a.B = std::min(per, B - b);
     a.x = static_cast<const uint16_t*>(x_dev) + (size_t)b * x_stride;
     a.y = static_cast<uint8_t*>(y_dev) + (size_t)b * y_stride * ysize;
     const int nt = (a.B + 1) / 2;
-    const RowsPlan p = plan_rows((N + 15) / 16, K, a.B, words, nt, w->zeros != nullptr, sms, dev);
-    a.S = p.S; a.WM = p.WM; a.WK = p.WK; a.R = p.R;
+    const RowsPlan p = plan_rows((N + 15) / 16, K, a.B, words, nt, sms, dev);
+    a.S = p.S; a.WM = p.WM; a.WK = p.WK; a.stages = p.stages; a.R = p.R;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     CKL(words == 4 ? launch_linear<4>(a, nt, p, dev, st) : words == 2 ? launch_linear<2>(a, nt, p, dev, st) : launch_linear<1>(a, nt, p, dev, st));
   }
@@ -243,8 +247,8 @@ prox_status_t prox_w4_stage2_ffn(const prox_w4_t* gate, const prox_w4_t* up, con
   a.list = list; a.count = count; a.n = most; a.members = members; a.h = h;
   a.hmax = reinterpret_cast<unsigned*>(wsp + ws.hmax);
   const int nt = (B + 1) / 2;
-  const RowsPlan p = plan_rows(std::max(1, (most + 7) / 8), D, B, 4, nt, gate->zeros != nullptr, std::min(sms, w4::kRowBlocks), dev);
-  a.S = p.S; a.WM = p.WM; a.WK = p.WK; a.R = p.R;
+  const RowsPlan p = plan_rows(std::max(1, (most + 7) / 8), D, B, 4, nt, std::min(sms, kMaxRowBlocks), dev);
+  a.S = p.S; a.WM = p.WM; a.WK = p.WK; a.stages = p.stages; a.R = p.R;
   CKL(gate->zeros ? launch_rows<4, true, true>(a, nt, p, dev, st) : launch_rows<4, false, true>(a, nt, p, dev, st));
   w4::DownArgs d = {};
   d.w = mat_of(down_t);

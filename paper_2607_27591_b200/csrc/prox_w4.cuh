@@ -4,12 +4,13 @@
 //   w[n, k] = s[n, k / G] (q[n, k] - z[n, k / G])          q 4 bits, s fp16, z an integer (8 where there are none)
 //   y[b, n] = sum_groups s[n, G] ( sum_{k in group} (q[n, k] - z) x[b, k] )
 //
-// The inner sum is a sum of whole numbers: a token's inputs are written as fixed-point numbers of 30 bits below the
+// The inner sum is a sum of whole numbers: a token's inputs are written as fixed-point numbers of 26 bits below the
 // token's largest, x = X 2^-e, and X as four signed base-256 digits, each a column of the B operand of the warp-level tensor-core
 // tile mma.sync m16n8k32 (u8 x s8 -> s32).  Eight codes become two u8 operands by a mask each, the low codes and 16 times the
 // high ones: two issue slots against nine in a 16-bit form (shift, four masks, four operations that take the
-// zero point off), and a tile step covers twice the columns.  Low and high codes have sums of their own, which start at what the
-// zero point takes off.  Sums are exact; scales enter in fp32 once per group.  All
+// zero point off), and a tile step covers twice the columns.  The low codes meet the digits of 16 X and the high ones, 16-fold
+// themselves, those of X, so that one sum takes both; it starts at what the zero point takes off.  Sums are exact; scales
+// enter in fp32 once per group.  All
 // kernels are to be bound by the weight stream: codes are read where the caller has them, once, and never written back in a
 // wider form.  What limits them next is the issue rate: while HBM delivers 1 KB to an SM it issues 177 instructions.  tcgen05
 // would want the codes unpacked in shared memory (it takes its operand from there): once in, once out and once in again
@@ -67,9 +68,10 @@ __device__ __forceinline__ uint2 ld8(const void* p) {
   return v;
 }
 
-__device__ __forceinline__ void mma(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+__device__ __forceinline__ void mma(int (&d)[4], const int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+      : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]));
 }
 
 // A byte holds two codes: the low ones of four bytes, and 16 times the high ones.
@@ -88,16 +90,16 @@ __device__ __forceinline__ void transpose(uint32_t (&r)[4], uint32_t a, uint32_t
   r[3] = __byte_perm(ab1, cd1, 0x7632);
 }
 
-// Fixed point of numbers up to the fp32 magnitude whose bits are `most`: times 2^e they are below 2^30.  What is not finite
+// Fixed point of numbers up to the fp32 magnitude whose bits are `most`: times 2^e they are below 2^26.  What is not finite
 // has no fixed point: its results are made NaN (scale_back).
-__device__ __forceinline__ int fixed_exponent(uint32_t most) { return 156 - max((int)(most >> 23), 1); }
+__device__ __forceinline__ int fixed_exponent(uint32_t most) { return 152 - max((int)(most >> 23), 1); }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
 __device__ __forceinline__ float times_pow2(float v, int e) {           // e in -250 .. 250
   const int a = max(-126, min(126, e));
   return v * pow2(a) * pow2(max(-126, min(126, e - a)));
 }
-__device__ __forceinline__ float scale_back(float v, uint32_t most) {
-  return most >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : times_pow2(v, -fixed_exponent(most));
+__device__ __forceinline__ float scale_back(float v, uint32_t most) {   // of 16 times a sum
+  return most >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : times_pow2(v, -fixed_exponent(most) - 4);
 }
 
 __device__ __forceinline__ void store(void* y, size_t i, float v, int type) {
@@ -135,6 +137,16 @@ __device__ __forceinline__ float cluster_read(const float* p, int rank) {   // a
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(r) : "memory");
   return v;
 }
+// Sum of that float over the S blocks of the cluster (at most 8), in their order; all reads under way at once.
+__device__ __forceinline__ float cluster_total(const float* p, int S) {
+  float v[8];
+#pragma unroll
+  for (int w = 0; w < 8; ++w) v[w] = w < S ? cluster_read(p, w) : 0.f;
+  float sum = v[0];
+#pragma unroll
+  for (int w = 1; w < 8; ++w) sum += v[w];
+  return sum;
+}
 __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
@@ -151,7 +163,8 @@ __device__ __forceinline__ void cluster_barrier() {
 // ----------------------------------------------------------------------------
 constexpr int kRowThreads = 512;
 constexpr int kRowWarps = kRowThreads / 32;
-constexpr int kRing = 4;                 // chunks of a warp in flight (a batch): 512 threads x 4 x 32 bytes = 64 KB per SM
+constexpr int kBatch = 2;                // chunks that a warp asks for at a time: a 128-byte line of each of 16 rows
+constexpr int kMaxStages = 5;            // batches of a warp in shared memory, at most (sid has room for them)
 constexpr int kMaxPass = 8;              // tokens of a pass over the weights: 32 columns of digits
 
 struct RowsArgs {
@@ -169,34 +182,31 @@ struct RowsArgs {
   const uint8_t* members;  // bit b: token b keeps the channel (null: one token)
   float* h;                // see emit
   unsigned* hmax;          // [blocks][B] bits of the largest |h| that a block has written
-  int S, WM, WK, R;        // R: units whose partial sums a block keeps before the cluster adds them up
+  int S, WM, WK, stages, R;   // R: units whose partial sums a block keeps before the cluster adds them up
   int x_half;              // x is fp16 (else bf16)
   int x_vec;               // x rows start on 16-byte boundaries
 };
 
-struct Codes { uint32_t q[2][4]; };      // what a lane holds of its two rows and a chunk
-
-// A warp's scales and zero points of a batch, 16 rows: bytes of a row (with room for where an element lies in its word)
+// A warp's stage: a batch of its 16 rows (codes with a gap behind every row, so that lanes of one load do not meet), their scales
+// and zero points (with room for where an element lies in its word).
 template <int W>
-struct Side {
-  static constexpr int kGroups = kRing * 4 / W;
-  static constexpr int kScales = W == 4 ? 16 : W == 2 ? 32 : 48;
-  static constexpr int kZeros = W == 4 ? 8 : W == 2 ? 16 : 32;
+struct Stage {
+  static constexpr int kGroups = kBatch * 4 / W;
+  static constexpr int kPitch = kBatch * 64 + 16 * W;
+  static constexpr int kScales = W == 4 ? 8 : W == 2 ? 16 : 32;         // bytes of a row
+  static constexpr int kZeros = W == 1 ? 16 : 8;
+  static constexpr int kAtScales = 16 * kPitch, kAtZeros = kAtScales + 16 * kScales, kBytes = kAtZeros + 16 * kZeros;
 };
-__host__ __device__ constexpr int rows_side_bytes(int words, bool zp) {   // of a warp, two batches
-  return 2 * 16 * ((words == 4 ? 16 : words == 2 ? 32 : 48) + (zp ? words == 4 ? 8 : words == 2 ? 16 : 32 : 0));
-}
+__host__ __device__ constexpr int rows_stage_bytes(int words) { return words == 4 ? Stage<4>::kBytes : words == 2 ? Stage<2>::kBytes : Stage<1>::kBytes; }
 
 // Chunks of a block of a cluster, of a warp along the columns: whole batches
-__host__ __device__ constexpr int rows_share(int C, int S) { return S == 1 ? C : ((C + S - 1) / S + kRing - 1) / kRing * kRing; }
-__host__ __device__ constexpr int rows_run(int Cs, int WK) { return ((Cs + WK - 1) / WK + kRing - 1) / kRing * kRing; }
+__host__ __device__ constexpr int rows_share(int C, int S) { return S == 1 ? C : ((C + S - 1) / S + kBatch - 1) / kBatch * kBatch; }
+__host__ __device__ constexpr int rows_run(int Cs, int WK) { return ((Cs + WK - 1) / WK + kBatch - 1) / kBatch * kBatch; }
 
-// Shared memory behind the tokens' digits: where a group's sums start, warps' scales, warps' partial tiles, the block's sums.
-// Start of a column pair (2 i, 2 i + 1) of a group, low and high codes: with zero points the sums of the digits that a zero
-// point multiplies (4 words); else what the zero point 8 takes off, as the four C registers of either sum (8 words)
+// Shared memory behind the tokens' digits: what comes off a group's sums, the warps' stages, their partial tiles, the block's sums
 __host__ __device__ constexpr size_t rows_digit_bytes(int chunks, int nt) { return (size_t)chunks * 1024 * nt; }
-__host__ __device__ constexpr size_t rows_fixed_bytes(int chunks, int nt, int words, bool zp) {
-  return rows_digit_bytes(chunks, nt) + (size_t)chunks * (4 / words) * 4 * nt * (zp ? 16 : 32) + (size_t)kRowWarps * rows_side_bytes(words, zp);
+__host__ __device__ constexpr size_t rows_fixed_bytes(int chunks, int nt, int words) {
+  return rows_digit_bytes(chunks, nt) + (size_t)chunks * (4 / words) * 64 * nt;
 }
 __host__ __device__ constexpr size_t rows_red_bytes(int nt) { return (size_t)2 * kRowWarps * nt * 512; }   // only where WK > 1
 
@@ -218,19 +228,20 @@ template <int W, int NT, bool ZP, bool GATEUP>
 __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) {
   extern __shared__ __align__(16) uint8_t rows_smem[];
   __shared__ unsigned xmax[kMaxPass], hm[kMaxPass];            // bits of the largest magnitude of a token's inputs, of its h
-  __shared__ int sid[3][GATEUP ? kRowWarps * 8 : 1];           // per unit (three alive at a time) and channel: what emit needs of it
+  __shared__ int sid[8][GATEUP ? kRowWarps * 8 : 1];           // per unit (those on their way, and the last) and channel: the tokens that keep it
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int S = a.S, WM = a.WM, WK = a.WK, B = a.B;
-  constexpr int cols = 8 * NT, pairs = 4 * NT;                 // of digits: two tokens a step of 8 (behind the last token: whatever is there, never used)
+  constexpr int cols = 8 * NT;                                 // of digits: two tokens a step of 8 (behind the last token: whatever is there, never used)
   const int rank = blockIdx.x % S, cid = blockIdx.x / S, ncl = gridDim.x / S;
   const int C = (a.K + 127) / 128, Cs = rows_share(C, S);
   const int cb0 = min(C, rank * Cs), cb1 = min(C, cb0 + Cs);
   constexpr int kTile = NT * 128;                              // a warp's partial tile: [NT][16 rows][8 columns]
   uint4* xs = reinterpret_cast<uint4*>(rows_smem);             // [chunk][two words of a lane][column][t]
-  int4* sx = reinterpret_cast<int4*>(rows_smem + rows_digit_bytes(Cs, NT));   // [group][pair of columns][1 or 2]
-  uint8_t* side = rows_smem + rows_fixed_bytes(Cs, NT, W, ZP) - (kRowWarps - warp) * rows_side_bytes(W, ZP);   // this warp's, two batches
-  const uint32_t side_at = (uint32_t)__cvta_generic_to_shared(side);
-  float* red = reinterpret_cast<float*>(rows_smem + rows_fixed_bytes(Cs, NT, W, ZP));   // [2][warps][kTile] (WK > 1)
+  float* sx = reinterpret_cast<float*>(rows_smem + rows_digit_bytes(Cs, NT));   // [group][column], or C registers [group][pair of columns][4]
+  using St = Stage<W>;
+  uint8_t* stages = rows_smem + rows_fixed_bytes(Cs, NT, W) + warp * a.stages * St::kBytes;   // this warp's
+  const uint32_t stages_at = (uint32_t)__cvta_generic_to_shared(stages);
+  float* red = reinterpret_cast<float*>(rows_smem + rows_fixed_bytes(Cs, NT, W) + kRowWarps * a.stages * St::kBytes);   // [2][warps][kTile] (WK > 1)
   float* part = red + (WK > 1 ? 2 * kRowWarps * kTile : 0);    // [R][B][WM * 16] (S > 1)
   if (tid < kMaxPass) xmax[tid] = hm[tid] = 0;
   __syncthreads();
@@ -238,13 +249,13 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) 
   dep_launch();
   constexpr int kPer = GATEUP ? 8 : 16;                        // list entries of a tile
   const int wm = warp / WK, wk = warp - wm * WK;
-  int id_next = 0;                                             // GATEUP: channel, and its tokens' bits from bit 20 on; 0 if it is none
+  int id_next = -1, bits_next = 1;                             // GATEUP: a channel and its tokens' bits, as they are in the lists
   auto entry = [&](int u) { return ((cid + u * ncl) * WM + wm) * kPer + g; };   // list entry of this lane's first row
-  auto fetch_id = [&](int u) {                                 // a channel id is read one unit ahead of its rows
-    if (GATEUP) {
-      const int pos = min(entry(u), max(a.n - 1, 0)), id = a.n > 0 ? a.list[pos] : -1;   // (an id behind the list's end is not used)
-      const int tokens = a.members ? a.members[pos] : 1;
-      id_next = (unsigned)id < (unsigned)a.rows ? id | tokens << 20 : 0;
+  auto fetch_id = [&](int u) {                                 // asked for one unit ahead of its rows, and not looked at before
+    if (GATEUP && a.n > 0) {
+      const int pos = min(entry(u), a.n - 1);                  // (an entry behind the list's end is not used)
+      id_next = a.list[pos];
+      if (a.members) bits_next = a.members[pos];
     }
   };
   if (wm < WM) fetch_id(0);
@@ -260,208 +271,234 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) 
   }
   const int nu = (U - cid - 1) / ncl + 1;
 
-  const int cw = rows_run(Cs, WK), nb = cw / kRing;            // chunks and batches of a warp and unit (the last warps may have fewer)
+  const int cw = rows_run(Cs, WK), nb = cw / kBatch;           // chunks and batches of a warp and unit (the last warps may have fewer)
   const int c0 = cb0 + wk * cw, c1 = wm < WM ? min(cb1, c0 + cw) : c0;
 
-  // loading side: unit lu (of this cluster's units), batch lb of it
-  int lu = 0, lb = 0;
-  const uint8_t *q0 = nullptr, *q1 = nullptr;                  // the lane's two rows, at the batch
-  int r0 = 0, r1 = 0;                                          // their numbers
+  // loading side: unit lu (of this cluster's units), batch lb of it, into stage lslot
+  int lu = 0, lb = 0, lslot = 0;
+  constexpr int kG = St::kGroups, kWordsS = (2 * kG + 5) / 4, kWordsZ = (kG + 6) / 4;
+  const bool aligned = a.groups % kG == 0;                     // scales of a batch of any row can be copied in one piece
+  int r0 = 0, r1 = 0;                                          // numbers of rows g and g + 8 of the tile
+  const uint8_t* rows[4];                                      // rows lane / 8, + 4, + 8, + 12 of the tile, at the lane's 16 bytes of a batch
+  const __half* side = nullptr;                                // scales of row lane % 16
+  const uint8_t* zside = nullptr;
+  const int half = a.K / 2, piece = (lane & 7) * 16;
+  const int gi0 = a.gstep ? c0 * (4 / W) : 0;
+  __shared__ uint8_t shifts[kRowWarps][8][16];                 // of a warp's units on their way: where in its word a row's first element lies
   auto open_unit = [&]() {
     if (GATEUP) {
-      r0 = r1 = id_next & 0xfffff;
-      if (wk == 0 && t == 0) sid[lu % 3][wm * 8 + g] = id_next;
+      const bool known = (unsigned)id_next < (unsigned)a.rows;
+      r0 = r1 = known ? id_next : 0;
+      if (wk == 0 && t == 0) sid[lu & 7][wm * 8 + g] = known ? bits_next : 0;
       if (lu + 1 < nu) fetch_id(lu + 1);
     } else {
       r0 = min(entry(lu), a.rows - 1);
       r1 = min(entry(lu) + 8, a.rows - 1);
     }
-    q0 = a.w.codes + (size_t)r0 * (a.K / 2) + (size_t)c0 * 64 + t * (4 * W);
-    q1 = (GATEUP ? a.w2.codes : a.w.codes) + (size_t)r1 * (a.K / 2) + (size_t)c0 * 64 + t * (4 * W);
-  };
-  // Codes of chunk d of batch lb.  A batch inside the row is read without any check; in the last one of a ragged row, what lies
-  // behind the row or the warp's chunks is read again from the row's start and meets digits that are 0, or is not used.
-  const int whole = min(c1, a.K / 128);                        // chunks before this one lie inside the row
-  auto load = [&](Codes& b, int d, bool inside) {
 #pragma unroll
-    for (int j = 0; j < 4 / W; ++j) {
-      int at = d * 64 + j * (16 * W);
-      if (!inside) {
-        const int k = (c0 + lb * kRing + d) * 128 + j * (32 * W) + t * (8 * W);
-        if (k >= a.K || c0 + lb * kRing + d >= c1) at = -((c0 + lb * kRing) * 64 + t * (4 * W));
-      }
-      if (W == 4) {
-        const uint4 v0 = ld16(q0 + at), v1 = ld16(q1 + at);
-        b.q[0][0] = v0.x; b.q[0][1] = v0.y; b.q[0][2] = v0.z; b.q[0][3] = v0.w;
-        b.q[1][0] = v1.x; b.q[1][1] = v1.y; b.q[1][2] = v1.z; b.q[1][3] = v1.w;
-      } else if (W == 2) {
-        const uint2 v0 = ld8(q0 + at), v1 = ld8(q1 + at);
-        b.q[0][2 * j] = v0.x; b.q[0][2 * j + 1] = v0.y;
-        b.q[1][2 * j] = v1.x; b.q[1][2 * j + 1] = v1.y;
-      } else {
-        b.q[0][j] = ld4(q0 + at);
-        b.q[1][j] = ld4(q1 + at);
-      }
+    for (int p = 0; p < 4; ++p) {
+      const int i = (p & 1) * 4 + (lane >> 3), r = __shfl_sync(0xffffffffu, p < 2 ? r0 : r1, i * 4);
+      rows[p] = (GATEUP && p >= 2 ? a.w2.codes : a.w.codes) + (size_t)r * half + (size_t)c0 * 64 + piece;
+    }
+    const int x0 = __shfl_sync(0xffffffffu, r0, (lane & 7) * 4), x1 = __shfl_sync(0xffffffffu, r1, (lane & 7) * 4);
+    const long long first = (long long)(lane & 8 ? x1 : x0) * a.groups + gi0;
+    side = (GATEUP && lane & 8 ? a.w2.scales : a.w.scales) + first;
+    if (ZP) zside = (GATEUP && lane & 8 ? a.w2.zeros : a.w.zeros) + first;
+    if (lane < 16) shifts[warp][lu & 7][lane] = (uint8_t)(first & 3);
+  };
+  // What a batch needs that is not whole or not aligned: the row's end, scales in the words that hold them
+  auto issue_ragged = [&](uint32_t to, int at) {
+    // (what lies behind the row or the warp's columns is left as it is: it meets digits that are 0, or is not used)
+    if (c0 * 64 + at + piece < min(half, c1 * 64)) {
+#pragma unroll
+      for (int p = 0; p < 4; ++p) copy16(to + (p * 4 + (lane >> 3)) * St::kPitch + piece, rows[p] + at);
+    }
+    const long long bytes = (long long)a.rows * a.groups * 2;
+    const int ahead = a.gstep ? lb * kG : 0;
+#pragma unroll 1
+    for (int e = lane; e < 16 * kWordsS + lane; e += 32) {     // (all lanes take every turn)
+      const int i = e / kWordsS & 15, w = e % kWordsS;
+      const uint8_t* base = reinterpret_cast<const uint8_t*>(GATEUP && i >= 8 ? a.w2.scales : a.w.scales);
+      const int x0 = __shfl_sync(0xffffffffu, r0, (i & 7) * 4), x1 = __shfl_sync(0xffffffffu, r1, (i & 7) * 4);
+      const long long from = (((long long)(i < 8 ? x0 : x1) * a.groups + gi0 + ahead) * 2 & ~3LL) + w * 4;
+      if (e < 16 * kWordsS) copy4(to + St::kAtScales + i * St::kScales + w * 4, base + (from < bytes ? from : 0), from < bytes ? (int)min(4LL, bytes - from) : 0);
     }
   };
-  // Scales and zero points of batch lb of the tile's 16 rows, copied to shared memory: whole where every row's start is aligned
-  // for it, else the words that hold them (a row's elements then start somewhere in its first word: `shift`)
-  using Sd = Side<W>;
-  constexpr int kG = Sd::kGroups, kWordsS = (2 * kG + 5) / 4, kWordsZ = (kG + 6) / 4;
-  auto load_side = [&](int buffer) {
-    const int gi = a.gstep ? (c0 + lb * kRing) * (4 / W) : 0;
-    const uint32_t to = side_at + buffer * (rows_side_bytes(W, ZP) / 2), to_z = to + 16 * Sd::kScales;
-    const bool whole_rows = a.groups % (ZP ? kG : kG < 8 ? kG : 8) == 0 && gi + kG <= a.groups;
-    // lanes 4 i hold the numbers of rows i and i + 8
-    auto row_of = [&](int i) {
+  auto issue_zeros = [&](uint32_t to) {
+    const long long bytes = (long long)a.rows * a.groups;
+    const int ahead = a.gstep ? lb * kG : 0;
+#pragma unroll 1
+    for (int e = lane; e < 16 * kWordsZ + lane; e += 32) {
+      const int i = e / kWordsZ & 15, w = e % kWordsZ;
+      const uint8_t* base = GATEUP && i >= 8 ? a.w2.zeros : a.w.zeros;
       const int x0 = __shfl_sync(0xffffffffu, r0, (i & 7) * 4), x1 = __shfl_sync(0xffffffffu, r1, (i & 7) * 4);
-      return i < 8 ? x0 : x1;
-    };
-    auto mat_of = [&](int i) -> const Mat& { return GATEUP && i >= 8 ? a.w2 : a.w; };
-    if (whole_rows) {
-      const int i = W == 1 ? lane >> 1 : lane & 15;
-      const long long at = (long long)row_of(i) * a.groups + gi;
-      if (W == 4 && lane < 16) copy8(to + i * Sd::kScales, mat_of(i).scales + at);
-      if (W == 2 && lane < 16) copy16_l1(to + i * Sd::kScales, mat_of(i).scales + at);
-      if (W == 1) copy16_l1(to + i * Sd::kScales + (lane & 1) * 16, mat_of(i).scales + at + (lane & 1) * 8);
-      if (ZP) {
-        if (W == 4 && lane < 16) copy4(to_z + i * Sd::kZeros, mat_of(i).zeros + at);
-        if (W == 2 && lane < 16) copy8(to_z + i * Sd::kZeros, mat_of(i).zeros + at);
-        if (W == 1 && !(lane & 1)) copy16_l1(to_z + i * Sd::kZeros, mat_of(i).zeros + at);
-      }
-    } else {
-      const long long bytes = (long long)a.rows * a.groups * 2;
+      const long long from = (((long long)(i < 8 ? x0 : x1) * a.groups + gi0 + ahead) & ~3LL) + w * 4;
+      if (e < 16 * kWordsZ) copy4(to + St::kAtZeros + i * St::kZeros + w * 4, base + (from < bytes ? from : 0), from < bytes ? (int)min(4LL, bytes - from) : 0);
+    }
+  };
+  const int whole_batches = max(0, min(c1, a.K / 128) - c0) / kBatch;   // batches of a unit that are inside the row
+  auto issue = [&]() {                                         // the next batch; nothing behind the last one
+    if (lu < nu) {
+      const uint32_t to = stages_at + lslot * St::kBytes;
+      const int at = lb * (kBatch * 64);
+      if (aligned && lb < whole_batches) {
 #pragma unroll
-      for (int p = 0; p < (16 * kWordsS + 31) / 32; ++p) {
-        const int e = p * 32 + lane, i = e / kWordsS & 15, w = e % kWordsS;
-        const long long at = (((long long)row_of(i) * a.groups + gi) * 2 & ~3LL) + w * 4;
-        if (e < 16 * kWordsS)
-          copy4(to + i * Sd::kScales + w * 4, reinterpret_cast<const uint8_t*>(mat_of(i).scales) + (at < bytes ? at : 0), at < bytes ? (int)min(4LL, bytes - at) : 0);
-      }
-      if (ZP) {
-        const long long zbytes = bytes / 2;
-#pragma unroll
-        for (int p = 0; p < (16 * kWordsZ + 31) / 32; ++p) {
-          const int e = p * 32 + lane, i = e / kWordsZ & 15, w = e % kWordsZ;
-          const long long at = (((long long)row_of(i) * a.groups + gi) & ~3LL) + w * 4;
-          if (e < 16 * kWordsZ) copy4(to_z + i * Sd::kZeros + w * 4, mat_of(i).zeros + (at < zbytes ? at : 0), at < zbytes ? (int)min(4LL, zbytes - at) : 0);
+        for (int p = 0; p < 4; ++p) copy16(to + (p * 4 + (lane >> 3)) * St::kPitch + piece, rows[p] + at);
+        if (lane < 16) {
+          const uint32_t dst = to + St::kAtScales + lane * St::kScales;
+          if (W == 4) copy4(dst, side + lb * kG);
+          else if (W == 2) copy8(dst, side + lb * kG);
+          else copy16_l1(dst, side + lb * kG);
+          if (ZP && W == 2) copy4(to + St::kAtZeros + lane * St::kZeros, zside + lb * kG);
+          if (ZP && W == 1) copy8(to + St::kAtZeros + lane * St::kZeros, zside + lb * kG);
         }
+        if (ZP && W == 4) issue_zeros(to);                     // (two zero points a row: half a word)
+      } else {
+        issue_ragged(to, at);
+        if (ZP) issue_zeros(to);
+      }
+      if (++lslot == a.stages) lslot = 0;
+      if (++lb == nb) {
+        lb = 0;
+        if (++lu < nu) open_unit();
       }
     }
     copies_end();
-    // byte offsets of this lane's rows in their first words: scales of row g and g + 8, zero points of row g and g + 8
-    const unsigned e0 = (unsigned)r0 * (unsigned)a.groups + gi, e1 = (unsigned)r1 * (unsigned)a.groups + gi;
-    return (e0 & 1) * 2 | (e1 & 1) << 9 | (e0 & 3) << 16 | (e1 & 3) << 24;
-  };
-  auto advance = [&]() {                                       // to the next batch (behind the last one: that again)
-    if (lb + 1 < nb) {
-      ++lb;
-      q0 += kRing * 64;
-      q1 += kRing * 64;
-    } else if (lu + 1 < nu) {
-      ++lu;
-      lb = 0;
-      open_unit();
-    }
   };
 
-  // The tokens' digits, in the order in which lanes take them.  Of a code word, columns 0, 2, 4, 6 are the low codes
-  // (b0) and 1, 3, 5, 7 the high ones (b1).  Two passes over x: the largest magnitude, then the digits; the first few
-  // inputs of a thread stay in registers in between.
-  Codes ring[kRing];
-  uint32_t shift_now = 0;
+  // The tokens' digits, in the order in which lanes take them.  Of a code word, columns 0, 2, 4, 6 are the low codes and
+  // 1, 3, 5, 7 the high ones; a 16-byte entry is the low ones of two words, then their high ones.  First the raw inputs, to the
+  // place of their own digits, and the largest magnitudes; then the digits.
   {
-    const int octets = (cb1 - cb0) * 16, items = octets * B;
-    constexpr int kKeep = 4;
-    uint4 keep[kKeep];
-    auto read = [&](int i) {
-      const int b = i / octets, k = cb0 * 128 + (i - b * octets) * 8;
-      if (k >= a.K) return make_uint4(0, 0, 0, 0);
-      const uint16_t* p = a.x + (size_t)b * a.x_stride + k;
-      if (a.x_vec) return __ldg(reinterpret_cast<const uint4*>(p));
-      uint32_t e[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) e[j] = __ldg(p + j);
-      return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+    // item: 16 inputs of the columns of two words of a lane t; its raw inputs first lie where its digits 0 and 1 go
+    const int items = (cb1 - cb0) * 8;
+    auto place = [&](int o, int b) {
+      const int c = o >> 3, r = o & 7, ot = W == 1 ? r & 3 : W == 2 ? r & 3 : r >> 1, p = W == 1 ? r >> 2 : W == 2 ? r >> 2 : r & 1;
+      return xs + ((c * 2 + p) * cols + b * 4) * 4 + ot;       // digit d 4 d further on
     };
-    auto raise = [&](int i, const uint4& v) {
-      float f[8];
-      inputs_of(f, v, a.x_half);
-      unsigned m = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(f[j]) & 0x7fffffffu);
-      if (m > xmax[i / octets]) atomicMax(xmax + i / octets, m);
+    auto column = [&](int o, int h) {                          // first input of the item's first or second word
+      const int c = cb0 + (o >> 3), r = o & 7;
+      return c * 128 + (W == 1 ? (r >> 2) * 64 + h * 32 + (r & 3) * 8 : r * 16 + h * 8);
     };
-    auto write = [&](int i, const uint4& v) {
-      const int b = i / octets, o = i - b * octets, e = fixed_exponent(xmax[b]);
-      float f[8];
-      inputs_of(f, v, a.x_half);
-      uint32_t d[8];
+    unsigned most[2 * NT];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) d[j] = digits(__float2int_rn(times_pow2(f[j], e)));
-      uint32_t lo[4], hi[4];
-      transpose(lo, d[0], d[2], d[4], d[6]);
-      transpose(hi, d[1], d[3], d[5], d[7]);
-      const int c = o >> 4, oc = o & 15;
-      const int ot = W == 4 ? oc >> 2 : W == 2 ? (oc & 7) >> 1 : oc & 3;
-      const int oi = W == 4 ? oc & 3 : W == 2 ? (oc >> 3) * 2 + (oc & 1) : oc >> 2;
-      uint2* at = reinterpret_cast<uint2*>(xs + ((c * 2 + (oi >> 1)) * cols + b * 4) * 4 + ot) + (oi & 1);
+    for (int b = 0; b < 2 * NT; ++b) most[b] = 0;
+#pragma unroll 1
+    for (int e = tid; e < items * 2; e += kRowThreads) {       // an item's first word, its second word
+      const int o = e >> 1, h = e & 1, k = column(o, h);
+      uint4 v[2 * NT];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) at[j * 8] = make_uint2(lo[j], hi[j]);
-    };
+      for (int b = 0; b < 2 * NT; ++b) {
+        v[b] = make_uint4(0, 0, 0, 0);
+        if (b < B && k < a.K && a.x_vec) v[b] = __ldg(reinterpret_cast<const uint4*>(a.x + (size_t)b * a.x_stride + k));
+      }
+      if (!a.x_vec && k < a.K) {
+#pragma unroll 1
+        for (int b = 0; b < B; ++b) {
+          const uint16_t* p = a.x + (size_t)b * a.x_stride + k;
+          const uint4 u = make_uint4(p[0] | (uint32_t)p[1] << 16, p[2] | (uint32_t)p[3] << 16, p[4] | (uint32_t)p[5] << 16, p[6] | (uint32_t)p[7] << 16);
 #pragma unroll
-    for (int j = 0; j < kKeep; ++j)
-      if (tid + j * kRowThreads < items) keep[j] = read(tid + j * kRowThreads);
+          for (int i = 0; i < 2 * NT; ++i)
+            if (i == b) v[i] = u;
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < 2 * NT; ++b) {
+        if (b < B) {
+          // (magnitudes of 16 bits order as whole numbers, and so do they once they are fp32 numbers)
+          const uint32_t m = __vmaxu2(__vmaxu2(v[b].x & 0x7fff7fffu, v[b].y & 0x7fff7fffu), __vmaxu2(v[b].z & 0x7fff7fffu, v[b].w & 0x7fff7fffu));
+          most[b] = max(most[b], max(m & 0xffffu, m >> 16));
+          place(o, b)[h * 4] = v[b];
+        }
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < 2 * NT; ++b) {
+      if (b < B) {
+        const unsigned m = __reduce_max_sync(0xffffffffu, most[b]);
+        const unsigned bits = a.x_half ? __float_as_uint(__half2float(__ushort_as_half((unsigned short)m))) : m << 16;
+        if (lane == 0 && m) atomicMax(xmax + b, bits);
+      }
+    }
     if (wm < WM) {                                             // the first weights: on their way meanwhile
       open_unit();
-#pragma unroll
-      for (int d = 0; d < kRing; ++d) load(ring[d], d, false);
-      shift_now = load_side(0);
+#pragma unroll 1
+      for (int d = 0; d < a.stages; ++d) issue();
     }
-#pragma unroll
-    for (int j = 0; j < kKeep; ++j)
-      if (tid + j * kRowThreads < items) raise(tid + j * kRowThreads, keep[j]);
-    for (int i = tid + kKeep * kRowThreads; i < items; i += kRowThreads) raise(i, read(i));
     __syncthreads();
+#pragma unroll 1
+    for (int i = tid; i < items * B; i += kRowThreads) {
+      const int b = i / items, o = i - b * items;
+      uint4* at = place(o, b);
+      const int e = fixed_exponent(xmax[b]);
+      uint32_t lo[2][4], hi[2][4];
+      const uint4 raw[2] = {at[0], at[4]};
 #pragma unroll
-    for (int j = 0; j < kKeep; ++j)
-      if (tid + j * kRowThreads < items) write(tid + j * kRowThreads, keep[j]);
-    for (int i = tid + kKeep * kRowThreads; i < items; i += kRowThreads) write(i, read(i));
+      for (int h = 0; h < 2; ++h) {
+        float f[8];
+        inputs_of(f, raw[h], a.x_half);
+        uint32_t d[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d[j] = digits(__float2int_rn(times_pow2(f[j], e)) << (j & 1 ? 0 : 4));   // the low codes' 16-fold
+        transpose(lo[h], d[0], d[2], d[4], d[6]);
+        transpose(hi[h], d[1], d[3], d[5], d[7]);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) at[j * 4] = make_uint4(lo[0][j], lo[1][j], hi[0][j], hi[1][j]);
+    }
   }
   __syncthreads();
-  // sums start at 1.5 2^23 as an fp32 number has it: with it the sum is the number's mantissa (|sum| <= 2^22)
-  constexpr int kBias = 0x4b400000;
-  for (int i = tid; i < (cb1 - cb0) * (4 / W) * pairs; i += kRowThreads) {
-    const int grp = i / pairs, pair = i - grp * pairs, c = grp / (4 / W), j = grp % (4 / W);
-    int lo[2] = {0, 0}, hi[2] = {0, 0};
+  // What comes off 16 times a group's sum: the zero point times the digits' sum of the group's high columns 16-fold and low
+  // columns: 8 times that, as the C registers that a lane's sums start with, or (zero points) that itself, in fp32.  (Below 2^24
+  // all: exact.)
+  for (int i = tid; i < (cb1 - cb0) * (4 / W) * cols; i += kRowThreads) {
+    const int grp = i / cols, col = i % cols, c = grp / (4 / W), j = grp % (4 / W);
+    int lo = 0, hi = 0;
+#pragma unroll 1
+    for (int oi = j * W; oi < (j + 1) * W; oi += 2)            // (a group of one word: half an entry)
 #pragma unroll
-    for (int w = 0; w < W; ++w)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int oi = j * W + w;
-          const uint2 v = *(reinterpret_cast<const uint2*>(xs + ((c * 2 + (oi >> 1)) * cols + pair * 2 + e) * 4 + q) + (oi & 1));
-          lo[e] = __dp4a((int)v.x, 0x01010101, lo[e]);
-          hi[e] = __dp4a((int)v.y, 0x01010101, hi[e]);
+      for (int q = 0; q < 4; ++q) {
+        const uint4 v = xs[((c * 2 + (oi >> 1)) * cols + col) * 4 + q];
+        if (W > 1 || !(oi & 1)) {
+          lo = __dp4a((int)v.x, 0x01010101, lo);
+          hi = __dp4a((int)v.z, 0x01010101, hi);
         }
-    if (ZP) {
-      sx[i] = make_int4(lo[0], lo[1], 16 * hi[0], 16 * hi[1]);
-    } else {
-      sx[2 * i] = make_int4(kBias - 8 * lo[0], kBias - 8 * lo[1], kBias - 8 * lo[0], kBias - 8 * lo[1]);
-      sx[2 * i + 1] = make_int4(kBias - 128 * hi[0], kBias - 128 * hi[1], kBias - 128 * hi[0], kBias - 128 * hi[1]);
-    }
+        if (W > 1 || oi & 1) {
+          lo = __dp4a((int)v.y, 0x01010101, lo);
+          hi = __dp4a((int)v.w, 0x01010101, hi);
+        }
+      }
+    const int sum = lo + 16 * hi;
+    if (ZP) sx[i] = (float)sum;
+    else reinterpret_cast<int*>(sx)[(i >> 1) * 4 + (i & 1)] = reinterpret_cast<int*>(sx)[(i >> 1) * 4 + 2 + (i & 1)] = -8 * sum;
   }
   __syncthreads();
 
   float acc[NT][4];
 #pragma unroll
   for (int i = 0; i < NT; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
-  auto compute = [&](const Codes& b, const uint8_t* sc, uint32_t shift, int c, int i4) {   // chunk c, i4 of its batch
+  auto compute = [&](const uint8_t* st, int e0, int e1, int c, int i2) {   // chunk c, i2 of the batch in st; e0, e1: where its rows' first words start
     const uint4* xc = xs + (c - cb0) * 8 * cols + g * 4 + t;
+    uint32_t q[2][4];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const uint8_t* from = st + (g + 8 * r) * St::kPitch + i2 * 64;
+#pragma unroll
+      for (int j = 0; j < 4 / W; ++j) {
+        if (W == 4) {
+          const uint4 v = *reinterpret_cast<const uint4*>(from + t * 16);
+          q[r][0] = v.x; q[r][1] = v.y; q[r][2] = v.z; q[r][3] = v.w;
+        } else if (W == 2) {
+          const uint2 v = *reinterpret_cast<const uint2*>(from + j * 32 + t * 8);
+          q[r][2 * j] = v.x; q[r][2 * j + 1] = v.y;
+        } else {
+          q[r][j] = *reinterpret_cast<const uint32_t*>(from + j * 16 + t * 4);
+        }
+      }
+    }
 #pragma unroll
     for (int j = 0; j < 4 / W; ++j) {
-      const int gi = a.gstep ? i4 * (4 / W) + j : 0;
+      const int gi = a.gstep ? i2 * (4 / W) + j : 0;
       // two words a step: the low codes of both, the high codes of both (a group of one word: the other half is zeros)
       uint32_t lw[(W + 1) / 2][4], hw[(W + 1) / 2][4];
 #pragma unroll
@@ -469,48 +506,45 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) 
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int word = j * W + 2 * p + (e >> 1);
-          const uint32_t q = W > 1 || e < 2 ? b.q[e & 1][word & 3] : 0u;
-          lw[p][e] = low_codes(q);
-          hw[p][e] = high_codes(q);
+          const uint32_t v = W > 1 || e < 2 ? q[e & 1][word & 3] : 0u;
+          lw[p][e] = low_codes(v);
+          hw[p][e] = high_codes(v);
         }
-      const uint8_t* sr = sc + g * Sd::kScales + gi * 2;
-      float f0 = __half2float(*reinterpret_cast<const __half*>(sr + (shift & 0xff))),
-            f1 = __half2float(*reinterpret_cast<const __half*>(sr + 8 * Sd::kScales + (shift >> 8 & 0xff)));
+      const __half* sr = reinterpret_cast<const __half*>(st + St::kAtScales + g * St::kScales) + gi;
+      float f0 = __half2float(sr[e0 & 1]), f1 = __half2float(sr[4 * St::kScales + (e1 & 1)]);
       if (W < 4 && c * (4 / W) + j >= a.groups) f0 = f1 = 0.f;  // behind the row (the sums are 0: so that a neighbour's scale does not matter)
-      int e0 = 0, e1 = 0;
+      float z0 = 0.f, z1 = 0.f;
       if (ZP) {
-        const uint8_t* zr = sc + 16 * Sd::kScales + g * Sd::kZeros + gi;
-        e0 = zr[shift >> 16 & 0xff];
-        e1 = zr[8 * Sd::kZeros + (shift >> 24)];
+        const uint8_t* zr = st + St::kAtZeros + g * St::kZeros + gi;
+        z0 = zr[e0];
+        z1 = zr[8 * St::kZeros + e1];
       }
 #pragma unroll
       for (int m = 0; m < NT; ++m) {
-        int lo[4], hi[4];
-        const int at = ((c - cb0) * (4 / W) + j) * pairs + m * 4 + t;
+        int d[4] = {0, 0, 0, 0};                               // 16 times the group's sums
+        float2 off = make_float2(0.f, 0.f);
+        const int at = ((c - cb0) * (4 / W) + j) * cols + m * 8 + 2 * t;
         if (ZP) {
-          const int4 v = sx[at];
-          lo[0] = kBias - e0 * v.x; lo[1] = kBias - e0 * v.y; lo[2] = kBias - e1 * v.x; lo[3] = kBias - e1 * v.y;
-          hi[0] = kBias - e0 * v.z; hi[1] = kBias - e0 * v.w; hi[2] = kBias - e1 * v.z; hi[3] = kBias - e1 * v.w;
+          off = *reinterpret_cast<const float2*>(sx + at);
         } else {
-          const int4 v = sx[2 * at], u = sx[2 * at + 1];
-          lo[0] = v.x; lo[1] = v.y; lo[2] = v.z; lo[3] = v.w;
-          hi[0] = u.x; hi[1] = u.y; hi[2] = u.z; hi[3] = u.w;
+          const int4 v = *reinterpret_cast<const int4*>(sx + at * 2);
+          d[0] = v.x; d[1] = v.y; d[2] = v.z; d[3] = v.w;
         }
 #pragma unroll
         for (int p = 0; p < (W + 1) / 2; ++p) {
-          const uint4 v = xc[((j * W + 2 * p) >> 1) * cols * 4 + m * 32];   // low, high columns of one word, of the other
+          const uint4 v = xc[((j * W + 2 * p) >> 1) * cols * 4 + m * 32];   // low columns of two words, high columns
           if (W > 1) {
-            mma(lo, lw[p][0], lw[p][1], lw[p][2], lw[p][3], v.x, v.z);
-            mma(hi, hw[p][0], hw[p][1], hw[p][2], hw[p][3], v.y, v.w);
+            mma(d, d, lw[p][0], lw[p][1], lw[p][2], lw[p][3], v.x, v.y);
+            mma(d, d, hw[p][0], hw[p][1], hw[p][2], hw[p][3], v.z, v.w);
           } else {
-            mma(lo, lw[p][0], lw[p][1], 0u, 0u, j & 1 ? v.z : v.x, 0u);
-            mma(hi, hw[p][0], hw[p][1], 0u, 0u, j & 1 ? v.w : v.y, 0u);
+            mma(d, d, lw[p][0], lw[p][1], hw[p][0], hw[p][1], j & 1 ? v.y : v.x, j & 1 ? v.w : v.z);
           }
         }
-        // (1.5 2^23 + low) + (1.5 2^23 + 16 high) / 16: whole numbers below 2^24, so exact
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          acc[m][e] = fmaf(e < 2 ? f0 : f1, fmaf(__int_as_float(hi[e]), 0.0625f, __int_as_float(lo[e])) - 13369344.f, acc[m][e]);
+        for (int e = 0; e < 4; ++e) {
+          const float v = ZP ? fmaf(e < 2 ? -z0 : -z1, e & 1 ? off.y : off.x, (float)d[e]) : (float)d[e];
+          acc[m][e] = fmaf(e < 2 ? f0 : f1, v, acc[m][e]);
+        }
       }
     }
   };
@@ -521,14 +555,14 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) 
     if (!GATEUP) {
       store(a.y, (size_t)b * a.y_stride + pos, v, a.y_type);
     } else {
-      int what;                                                // the channel's tokens, from bit 20 on
+      int what;                                                // the channel's tokens
       if (S == 1) {
-        what = sid[u % 3][r];
+        what = sid[u & 7][r];
       } else {                                                 // (a cluster ends several units at a time)
         const int id = a.list[pos];
-        what = (unsigned)id < (unsigned)a.rows ? (a.members ? a.members[pos] : 1) << 20 : 0;
+        what = (unsigned)id < (unsigned)a.rows ? a.members ? a.members[pos] : 1 : 0;
       }
-      const float h = what >> (20 + b) & 1 ? up * (v / (1.0f + expf(-v))) : 0.f;
+      const float h = what >> b & 1 ? up * (v / (1.0f + expf(-v))) : 0.f;
       // [tile of 32 entries][token][8 t + r]: entry r * 4 + t of the tile, as lanes t of the down projection take them
       a.h[((size_t)(pos >> 5) * B + b) * 32 + (pos & 3) * 8 + (pos >> 2 & 7)] = h;
       const unsigned m = __float_as_uint(h) & 0x7fffffffu;
@@ -542,12 +576,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) 
     for (int i = rank * kRowThreads + tid; i < units * outs; i += S * kRowThreads) {
       const int du = i / outs, j = i - du * outs, b = j / (WM * kPer), r = j - b * (WM * kPer);
       const float* p = part + du * (WM * 16 * B) + b * (WM * 16) + (GATEUP ? (r >> 3) * 16 + (r & 7) : r);
-      float v = 0.f, up = 0.f;
-      for (int w = 0; w < S; ++w) {
-        v += cluster_read(p, w);
-        if (GATEUP) up += cluster_read(p + 8, w);
-      }
-      emit(first + du, r, b, v, up);
+      emit(first + du, r, b, cluster_total(p, S), GATEUP ? cluster_total(p + 8, S) : 0.f);
     }
     cluster_barrier();                                         // nobody overwrites or leaves while another block reads
   };
@@ -608,32 +637,29 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) 
     if (S > 1 && ((u + 1) % a.R == 0 || u + 1 == nu)) cluster_sum(u);
   };
 
-  int buffer = 0;
+  int slot = 0;
+#pragma unroll 1
   for (int u = 0; u < nu; ++u) {
     if (wm < WM) {                                             // (others have no tile of their own)
+      int e0 = shifts[warp][u & 7][g], e1 = shifts[warp][u & 7][8 + g];
+#pragma unroll 1
       for (int batch = 0; batch < nb; ++batch) {
-        copies_wait<0>();
+        if (a.stages == kMaxStages) copies_wait<kMaxStages - 1>();
+        else if (a.stages == 3) copies_wait<2>();
+        else copies_wait<1>();
         __syncwarp();
-        advance();
-        const uint32_t shift_next = load_side(buffer ^ 1);
-        const uint8_t* sc = side + buffer * (rows_side_bytes(W, ZP) / 2);
-        const int c = c0 + batch * kRing;
-        if (c + kRing <= c1 && c0 + (lb + 1) * kRing <= whole) {   // (a batch without an end in it, and the next one to load)
+        const uint8_t* st = stages + slot * St::kBytes;
+        const int c = c0 + batch * kBatch;
+        if (c + kBatch <= c1) {
 #pragma unroll
-          for (int d = 0; d < kRing; ++d) {
-            compute(ring[d], sc, shift_now, c + d, d);
-            load(ring[d], d, true);
-          }
-        } else {
-#pragma unroll
-          for (int d = 0; d < kRing; ++d) {
-            if (c + d < c1) compute(ring[d], sc, shift_now, c + d, d);
-            load(ring[d], d, false);
-          }
+          for (int d = 0; d < kBatch; ++d) compute(st, e0, e1, c + d, d);
+        } else if (c < c1) {                                   // (kBatch is 2)
+          compute(st, e0, e1, c, 0);
         }
         __syncwarp();
-        shift_now = shift_next;
-        buffer ^= 1;
+        issue();
+        if (++slot == a.stages) slot = 0;
+        if (a.gstep) { e0 = (e0 + kG) & 3; e1 = (e1 + kG) & 3; }
       }
     }
     finish_unit(u);
@@ -664,21 +690,27 @@ union_kernel(const int* __restrict__ sel, int stride, const int* __restrict__ co
   dep_wait();
   dep_launch();
   __syncthreads();
-  constexpr int kAhead = 16;                                   // (entries of a thread on their way at a time)
-  const long long items = (long long)B * k2;
-  for (long long i = tid; i < items; i += kAhead * kUnionThreads) {
-    int id[kAhead], tok[kAhead];
+  constexpr int kAhead = 4;                                    // entries of every token that a thread asks for at a time
+  int lens[kMaxPass];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      const int e = (int)min(i + j * kUnionThreads, items - 1), b = e / k2, r = e - b * k2;
-      tok[j] = b;
-      id[j] = r < (count ? count[b] : k2) && i + j * kUnionThreads < items ? sel[(size_t)b * stride + r] : -1;
-    }
+  for (int b = 0; b < kMaxPass; ++b) lens[b] = b < B ? count ? max(0, min(k2, count[b])) : k2 : 0;
+#pragma unroll 1
+  for (int i = tid; i < k2; i += kAhead * kUnionThreads) {
+    int id[kMaxPass][kAhead];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      const int f = id[j] - f0;
-      if (id[j] >= 0 && (unsigned)f < (unsigned)nf) atomicOr(un_words + (f >> 2), 1u << (tok[j] + 8 * (f & 3)));
-    }
+    for (int b = 0; b < kMaxPass; ++b)
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        id[b][j] = -1;
+        if (i + j * kUnionThreads < lens[b]) id[b][j] = sel[(size_t)b * stride + i + j * kUnionThreads];
+      }
+#pragma unroll
+    for (int b = 0; b < kMaxPass; ++b)
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int f = id[b][j] - f0;
+        if (id[b][j] >= 0 && (unsigned)f < (unsigned)nf) atomicOr(un_words + (f >> 2), 1u << (b + 8 * (f & 3)));
+      }
   }
   __syncthreads();
   const int per = (words + kUnionThreads - 1) / kUnionThreads, w0 = min(words, tid * per), w1 = min(words, w0 + per);
@@ -730,15 +762,15 @@ union_kernel(const int* __restrict__ sel, int stride, const int* __restrict__ co
 //
 // M = columns, K = list entries, N = digits of the tokens' h s.  A warp owns 128 columns (one scale group) and takes
 // tiles of 32 entries: 64 bytes of each of 32 rows, copied to its own stages in shared memory with what else the tile needs
-// (scales, zero points, h); four rows' bytes are transposed into A registers.  h s is a fixed-point number of 30 bits below
-// the largest that the block can meet (the token's largest |h|, which the kernel before it has left, times the largest
-// scale of the block's rows), so one whole-number sum runs over all tiles: |digit| <= 128, 16 q <= 240, at most 32768
-// entries, below 2^30.
+// (scales, zero points, h); four rows' bytes are transposed into A registers.  h s is a fixed-point number, and one
+// whole-number sum runs over all tiles: |digit| <= 128, 16 q <= 240, at most 32768 entries, below 2^30.  Its exponent is the
+// warp's and the token's: 30 bits are room for the token's largest |h|, which the kernel before this has left, times four times
+// the largest scale of the warp's first tile.  Where a tile brings a scale above that, the exponents fall and the numbers
+// that the sums so far stand for are shifted down.
 // WC warps of a block are side by side in the columns (what they read of h and of the scales' sectors they share
 // through L1), the other warps and the S blocks of a cluster split the entries; their sums meet in the cluster's shared memory,
 // in a fixed order: results do not depend on timing.
 // ----------------------------------------------------------------------------
-constexpr int kRowBlocks = 256;          // of the gate and up kernel, at most (their largest |h|)
 __host__ __device__ constexpr int down_threads(int nt) { return nt >= 3 ? 256 : 512; }   // 32 sums a thread and 8 columns of digits
 __host__ __device__ constexpr int down_stages(int nt) { return nt >= 3 ? 6 : 4; }        // 12 KB of codes a warp in flight, or 8
 
@@ -759,12 +791,26 @@ struct DownArgs {
 // bytes of a stage: 32 rows of codes, a word each of scales, zero points and where to look in them, h
 __host__ __device__ constexpr int down_stage(int B) { return 2048 + 128 + 128 + 128 + 128 * B; }
 
+// The sums of the four digits of a number, two of them in this lane and two in the next (odd: the upper ones), for the number
+// shifted down by `by` bits, rounded; c[0], c[1] and c[2], c[3] belong to different numbers.
+__device__ __forceinline__ void shift_sums(int (&c)[4], int by, int odd) {
+#pragma unroll
+  for (int k = 0; k < 4; k += 2) {
+    const long long mine = c[k] + 256ll * c[k + 1], other = __shfl_xor_sync(0xffffffffu, mine, 1);
+    const long long v = odd ? other + mine * 65536 : mine + other * 65536, w = by ? (v + (1ll << (by - 1))) >> by : v;
+    const int low = (int)(w & 0xffff);                         // digits 0 and 1, what is left for 2 and 3
+    const long long high = w >> 16;
+    c[k] = odd ? (int)(high & 0xff) : low & 0xff;
+    c[k + 1] = odd ? (int)(high >> 8) : low >> 8;
+  }
+}
+
 template <int NT, bool ZP>
 __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArgs a) {
   extern __shared__ __align__(16) uint8_t down_smem[];
   constexpr int kThreads = down_threads(NT), kWarps = kThreads / 32, kStages = down_stages(NT);
-  __shared__ unsigned hm[kMaxPass], smax;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3, B = a.B;
+  __shared__ unsigned hm[kMaxPass];                            // bits of the tokens' largest |h|
   const int S = a.S, rank = blockIdx.x % S, slice = blockIdx.x / S;
   const int WC = a.WC, WR = kWarps / WC, wc = warp % WC, wr = warp / WC;
   const int cg = slice * WC + wc;                              // the warp's group of 128 columns
@@ -773,7 +819,6 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
   uint8_t* mine = down_smem + warp * (kStages * stage);
   const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
   if (tid < kMaxPass) hm[tid] = 0;
-  if (tid == kMaxPass) smax = 0;
   __syncthreads();
   // Up to dep_wait nothing is read that the gate and up kernel writes.  (What came before that kernel is complete: it has waited
   // for it before it let this one start.)
@@ -784,17 +829,11 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
   const int gi = cg * a.gstep;
   const long long all = (long long)a.F * a.groups;
 
-  // id of entry `lane` of a tile; entries behind the list repeat its last one (their h is not used)
-  auto fetch = [&](int tile) {
-    int id = 0;
-    if (tile < end) {
-      id = a.list[min(tile * 32 + lane, n - 1)];
-      if ((unsigned)id >= (unsigned)a.F) id = 0;
-    }
-    return id;
-  };
+  // id of entry `lane` of a tile, as it is in the list; entries behind the list repeat its last one (their h is not used)
+  auto fetch = [&](int tile) { return tile < end ? a.list[min(tile * 32 + lane, n - 1)] : 0; };
   auto issue = [&](int tile, int slot, int id) {
     if (tile < end) {
+      if ((unsigned)id >= (unsigned)a.F) id = 0;
       const uint32_t at = mine_at + slot * stage;
 #pragma unroll
       for (int p = 0; p < 4; ++p) {                            // row r at r * 64; its 16-byte pieces swapped so that lanes t do not meet
@@ -827,68 +866,24 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
 #pragma unroll
     for (int d = 0; d < kStages; ++d) issue(first + d * WR, d, ids[d]);
   }
-  // the largest scale of the block's rows and columns: WC scales of a row in one load where they are aligned for it
-  {
-    const int g0 = slice * WC * a.gstep, width = a.gstep ? min(WC, a.groups - g0) : 1;
-    const bool wide = width == WC && a.groups % WC == 0;
-    uint32_t most = 0;
-    constexpr int kAhead = 4;
-    for (int e = b0 * 32 + tid; e < min(n, b1 * 32); e += kAhead * kThreads) {
-      long long at[kAhead];
-#pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
-        int id = a.list[min(e + j * kThreads, n - 1)];
-        if ((unsigned)id >= (unsigned)a.F) id = 0;
-        at[j] = (long long)id * a.groups + g0;
-      }
-      if (wide && WC == 8) {
-        uint4 v[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) v[j] = __ldg(reinterpret_cast<const uint4*>(a.w.scales + at[j]));
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-          most = __vmaxu2(most, __vmaxu2(__vmaxu2(v[j].x & 0x7fff7fffu, v[j].y & 0x7fff7fffu), __vmaxu2(v[j].z & 0x7fff7fffu, v[j].w & 0x7fff7fffu)));
-      } else if (wide && WC == 4) {
-        uint2 v[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) v[j] = __ldg(reinterpret_cast<const uint2*>(a.w.scales + at[j]));
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) most = __vmaxu2(most, __vmaxu2(v[j].x & 0x7fff7fffu, v[j].y & 0x7fff7fffu));
-      } else {
-        for (int k = 0; k < width; ++k) {
-          unsigned v[kAhead];
-#pragma unroll
-          for (int j = 0; j < kAhead; ++j) v[j] = __half_as_ushort(__ldg(a.w.scales + at[j] + k));
-#pragma unroll
-          for (int j = 0; j < kAhead; ++j) most = __vmaxu2(most, v[j] & 0x7fffu);
-        }
-      }
-    }
-    most = __reduce_max_sync(0xffffffffu, max(most & 0xffffu, most >> 16));
-    if (lane == 0 && most) atomicMax(&smax, most);
-  }
   dep_wait();
   dep_launch();
 #pragma unroll
   for (int d = 0; d < kStages; ++d) issue_h(first + d * WR, d);
   copies_end();
+
   for (int i = tid; i < a.hblocks * B; i += kThreads) {
     const unsigned m = a.hmax[i];
     if (m > hm[i % B]) atomicMax(hm + i % B, m);
   }
   __syncthreads();
-
-  // the fixed point of every token: 30 bits below max |h| max s
-  const float top = __half2float(__ushort_as_half((unsigned short)smax));
-  auto most_of = [&](int b) { return __float_as_uint(__uint_as_float(hm[b]) * top) & 0x7fffffffu; };
-  auto exponent_of = [&](unsigned most) { return min(fixed_exponent(most) - 1, 126); };   // (the product is rounded: one bit of room)
-  int token[NT];
-  float factor[NT];
+  int token[NT], power[NT][2];                                 // fixed point of tokens 2 i and 2 i + 1: h s times 2^power
+  uint32_t most_scale = 0;                                     // bits of the scale that there is room for; 0: no sums yet
 #pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    token[i] = min(i * 2 + (g >> 2), B - 1);                   // columns behind the last token: computed, never used
-    factor[i] = pow2(exponent_of(most_of(token[i])));
-  }
+  for (int i = 0; i < NT; ++i) token[i] = min(i * 2 + (g >> 2), B - 1);   // columns behind the last token: computed, never used
+  auto power_of = [&](int b) {                                 // (of a product that is rounded: one bit of room)
+    return min(fixed_exponent(__float_as_uint(__uint_as_float(hm[min(b, B - 1)]) * __uint_as_float(most_scale)) & 0x7fffffffu) + 3, 126);
+  };
 
   int acc[8][NT][4], zacc[NT][4];                              // even columns (rows g): sums of q, odd ones (g + 8): of 16 q
 #pragma unroll
@@ -908,11 +903,30 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
     const float s0 = __half2float(__ushort_as_half((unsigned short)(sw.x >> ((odd >> (r0 * 4) & 1) << 4))));
     const float s1 = __half2float(__ushort_as_half((unsigned short)(sw.y >> ((odd >> (r0 * 4 + 4) & 1) << 4))));
     const bool in0 = tile * 32 + r0 * 4 + t < n, in1 = tile * 32 + r0 * 4 + 4 + t < n;
+    const uint32_t scale_bits = __reduce_max_sync(0xffffffffu, max(__float_as_uint(s0) & 0x7fffffffu, __float_as_uint(s1) & 0x7fffffffu));
+    if (scale_bits > most_scale) {                             // the first tile, seldom another
+      const bool sums = most_scale != 0;
+      most_scale = max(scale_bits, 0x33800000u) + 0x01000000u; // times 4 (at least 2^-24, fp16's least)
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        const int old[2] = {power[i][0], power[i][1]};
+        power[i][0] = power_of(2 * i);
+        power[i][1] = power_of(2 * i + 1);
+        if (sums) {                                            // a lane's sums are columns 2 t, 2 t + 1: of one token
+          const int by = min(t & 2 ? old[1] - power[i][1] : old[0] - power[i][0], 62);
+          shift_sums(zacc[i], by, t & 1);
+#pragma unroll
+          for (int m = 0; m < 8; ++m) shift_sums(acc[m][i], by, t & 1);
+        }
+      }
+    }
     uint32_t bf[NT][2];
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       const float2 h = *reinterpret_cast<const float2*>(st + 2432 + token[i] * 128 + t * 32 + r0 * 4);
-      const uint32_t d0 = digits(in0 ? __float2int_rn(h.x * factor[i] * s0) : 0), d1 = digits(in1 ? __float2int_rn(h.y * factor[i] * s1) : 0);
+      const float v0 = in0 ? h.x * s0 : 0.f, v1 = in1 ? h.y * s1 : 0.f;
+      const float factor = pow2(g < 4 ? power[i][0] : power[i][1]);
+      const uint32_t d0 = digits(__float2int_rn(v0 * factor)), d1 = digits(__float2int_rn(v1 * factor));
       // bytes 0, 1 of both numbers, and bytes 2, 3: lanes of digits 0, 1 keep the former and get those of the lane two further on
       const uint32_t low = __byte_perm(d0, d1, 0x5140), high = __byte_perm(d0, d1, 0x7362);   // (d0.0 d1.0 d0.1 d1.1), (.2 .2 .3 .3)
       const uint32_t keep = g & 2 ? high : low, got = __shfl_xor_sync(0xffffffffu, g & 2 ? low : high, 8);
@@ -939,7 +953,7 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
       }
     }
 #pragma unroll
-    for (int i = 0; i < NT; ++i) mma(zacc[i], zr[0], zr[0], zr[1], zr[1], bf[i][0], bf[i][1]);
+    for (int i = 0; i < NT; ++i) mma(zacc[i], zacc[i], zr[0], zr[0], zr[1], zr[1], bf[i][0], bf[i][1]);
     uint2 q[8];
 #pragma unroll
     for (int r = 0; r < 8; ++r) q[r] = *reinterpret_cast<const uint2*>(st + (r * 4 + t) * 64 + (((g >> 1) ^ (t & 2)) << 4) + (g & 1) * 8);
@@ -957,7 +971,7 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
       for (int m = 0; m < 4; ++m) {
         const uint32_t a0 = low_codes(lo[m]), a1 = high_codes(lo[m]), a2 = low_codes(hi[m]), a3 = high_codes(hi[m]);
 #pragma unroll
-        for (int i = 0; i < NT; ++i) mma(acc[hw * 4 + m][i], a0, a1, a2, a3, bf[i][0], bf[i][1]);
+        for (int i = 0; i < NT; ++i) mma(acc[hw * 4 + m][i], acc[hw * 4 + m][i], a0, a1, a2, a3, bf[i][0], bf[i][1]);
       }
     }
   };
@@ -985,9 +999,8 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     const int b = i * 2 + (t >> 1);                            // lane t has digits 0, 1 (t even) or 2, 3 (t odd) of the token
-    const unsigned most = b < B ? most_of(b) : 0u;
-    const int e = -exponent_of(most), e0 = max(-126, min(126, e));
-    const float f0 = most >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : pow2(e0), f1 = pow2(max(-126, min(126, e - e0)));
+    const int e = most_scale ? -(t & 2 ? power[i][1] : power[i][0]) : 0, e0 = max(-126, min(126, e));
+    const float f0 = hm[min(b, B - 1)] >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : pow2(e0), f1 = pow2(max(-126, min(126, e - e0)));
     float* at = red + (size_t)wr * outs + b * width + wc * 128 + g * 16 + (t & 1);
 #pragma unroll
     for (int m = 0; m < 8; ++m) {                              // columns g * 16 + 2 m (even lanes), + 1 (odd lanes) of the warp's
@@ -1011,8 +1024,7 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
   cluster_barrier();
   for (int i = rank * kThreads + tid; i < outs; i += S * kThreads) {
     const int b = i / width, d = slice * width + i - b * width;
-    float v = 0.f;
-    for (int w = 0; w < S; ++w) v += cluster_read(red + i, w);
+    const float v = cluster_total(red + i, S);
     if (d < a.D) store(a.y, (size_t)b * a.D + d, v, a.y_type);
   }
   cluster_barrier();                                           // nobody leaves while another block reads
