@@ -189,14 +189,6 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
     return *reinterpret_cast<const uint4*>(e);
   };
 
-  // the given tokens' logits, on their way from the start (the first kThreads of them)
-  float given_logit = 0.f;
-  int given = -1;
-  if (rank == 0 && tid < a.n_given) {
-    given = a.given[row * a.n_given + tid];
-    if (given >= 0 && given < a.V) given_logit = widen<DT>(reinterpret_cast<const T*>(start)[given]);
-  }
-
   if (TOP) {
     if (tid == 0) { count = 0; floor_now = __uint_as_float(0xff800000u); }
   }
@@ -207,6 +199,7 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
       const int i = i0 + tid / parts;
       const unsigned long long mine = i < n ? list[i] : ~0ull;
       int above = 0;
+#pragma unroll 8
       for (int j = tid % parts; j < n; j += parts) above += list[j] > mine;
       if (parts > 1) above += __shfl_xor_sync(0xffffffffu, above, 1);
       if (parts > 2) above += __shfl_xor_sync(0xffffffffu, above, 2);
@@ -220,15 +213,28 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
     }
     __syncthreads();
   };
-  auto each = [&](const uint4 (&v)[kVectors], int q, auto&& f) {     // all logits of a thread's vectors of a round
+  auto each = [&](const uint4 (&v)[kVectors], int q, float floor_v, auto&& f) {   // a thread's logits of a round that reach the floor
 #pragma unroll
     for (int j = 0; j < kVectors; ++j) {
-      float x[kPer];
+      float x[kPer], most = __uint_as_float(0xff800000u);
       widen<DT>(x, v[j]);
 #pragma unroll
+      for (int e = 0; e < kPer; ++e) most = max_nan(most, x[e]);
+      if (most < floor_v || q + j * kThreads >= q1) continue;
+      const int first = (q + j * kThreads) * kPer - head;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e)
+        if (!(x[e] < floor_v) && first + e >= 0 && first + e < a.V) f(x[e], first + e);
+    }
+  };
+  auto each_again = [&](int q, auto&& f) {                     // the same, read once more: short code for what happens seldom
+#pragma unroll 1
+    for (int j = 0; j < kVectors; ++j) {
+      const uint4 v = load(q + j * kThreads);
+      const T* x = reinterpret_cast<const T*>(&v);
       for (int e = 0; e < kPer; ++e) {
         const int index = (q + j * kThreads) * kPer + e - head;
-        if (q + j * kThreads < q1 && index >= 0 && index < a.V) f(x[e], index);
+        if (q + j * kThreads < q1 && index >= 0 && index < a.V) f(widen<DT>(x[e]), index);
       }
     }
   };
@@ -237,14 +243,32 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
   uint4 now[kVectors], next[kVectors];
 #pragma unroll
   for (int j = 0; j < kVectors; ++j) now[j] = load(q0 + tid + j * kThreads);
+
+  const int whole0 = max(q0, head ? 1 : 0), whole1 = min(q1, (head + a.V) / kPer);   // vectors that lie inside the row
+  const uint8_t* ahead = base + ((size_t)q0 + tid + kVectors * kThreads) * 16;       // the next round's
+
+  // the given tokens' logits, on their way behind the first round's (the first kThreads of them)
+  float given_logit = 0.f;
+  int given = -1;
+  if (rank == 0 && tid < a.n_given) {
+    given = a.given[row * a.n_given + tid];
+    if (given >= 0 && given < a.V) given_logit = widen<DT>(reinterpret_cast<const T*>(start)[given]);
+  }
+
   bool first_round = true;
   for (int qr = q0; qr < q1; qr += kVectors * kThreads) {
     const int q = qr + tid;
     const bool more = qr + kVectors * kThreads < q1;
-    if (more) {
+    if (qr + kVectors * kThreads >= whole0 && qr + 2 * kVectors * kThreads <= whole1) {
+#pragma unroll
+      for (int j = 0; j < kVectors; ++j)
+        asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(next[j].x), "=r"(next[j].y), "=r"(next[j].z), "=r"(next[j].w) : "l"(ahead + j * (kThreads * 16)));
+    } else if (more) {
 #pragma unroll
       for (int j = 0; j < kVectors; ++j) next[j] = load(q + (kVectors + j) * kThreads);
     }
+    ahead += kVectors * kThreads * 16;
     float most = __uint_as_float(0xff800000u);
 #pragma unroll
     for (int j = 0; j < kVectors; ++j) {
@@ -303,11 +327,9 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
       const float floor_v = floor_now;
       int end = 0;
       if (!(most < floor_v)) {
-        each(now, q, [&](float x, int index) {
-          if (!(x < floor_v)) {
-            end = atomicAdd(&count, 1) + 1;
-            if (end <= kList) list[end - 1] = key_of(x, index);
-          }
+        each(now, q, floor_v, [&](float x, int index) {
+          end = atomicAdd(&count, 1) + 1;
+          if (end <= kList) list[end - 1] = key_of(x, index);
         });
       }
       if (__syncthreads_or(end > kList / 2)) {
@@ -332,7 +354,7 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
           for (int i = 0; i < kList / kThreads; ++i)
             if (kept[i]) list[atomicAdd(&count, 1)] = kept[i];
           unsigned long long top = 0;
-          each(now, q, [&](float x, int index) { top = max(top, key_of(x, index)); });
+          each_again(q, [&](float x, int index) { top = max(top, key_of(x, index)); });
           __syncthreads();
           list[kList - kThreads + tid] = top;
           __syncthreads();
@@ -343,7 +365,7 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
           const unsigned long long least = best[0];
           __syncthreads();
           if (top >= least)
-            each(now, q, [&](float x, int index) {
+            each_again(q, [&](float x, int index) {
               const unsigned long long key = key_of(x, index);
               if (key >= least) list[atomicAdd(&count, 1)] = key;
             });
@@ -366,25 +388,29 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
   if (lane == 0) warp_sums[warp] = sum;
   __syncthreads();
   if (TOP) settle(count);
-  if (tid == 0) {
-    Sums all = warp_sums[0];
-    for (int w = 1; w < kWarps; ++w) all = join(all, warp_sums[w], c);
-    block_sums = all;
+  // of as many sums as there are (a power of two), one a lane of the first warp: joined in pairs
+  auto join_lanes = [&](Sums v, int n) {
+    for (int o = 1; o < n; o <<= 1) {
+      const Sums other = {__shfl_xor_sync(0xffffffffu, v.m, o), __shfl_xor_sync(0xffffffffu, v.s, o), __shfl_xor_sync(0xffffffffu, v.w, o)};
+      v = lane & o ? join(other, v, c) : join(v, other, c);
+    }
+    return v;
+  };
+  if (warp == 0) {
+    const Sums v = join_lanes(warp_sums[lane % kWarps], kWarps);
+    if (lane == 0) block_sums = v;
   }
   if (S > 1) {
     cluster_barrier();
     if (rank == 0) {
-      if (tid == 0) {
-        Sums all = block_sums;
-        for (int r = 1; r < S; ++r) {
-          const uint32_t at = cluster_address(&block_sums, r);
-          Sums o;
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.m) : "r"(at) : "memory");
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.s) : "r"(at + 4) : "memory");
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o.w) : "r"(at + 8) : "memory");
-          all = join(all, o, c);
-        }
-        warp_sums[0] = all;
+      if (warp == 0) {
+        const uint32_t at = cluster_address(&block_sums, lane % S);
+        Sums v;
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v.m) : "r"(at) : "memory");
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v.s) : "r"(at + 4) : "memory");
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v.w) : "r"(at + 8) : "memory");
+        v = join_lanes(v, S);
+        if (lane == 0) warp_sums[0] = v;
       }
       if (TOP) {
         for (int i = tid; i < (S - 1) * a.k; i += kThreads) {  // (a block may have had fewer logits than k)

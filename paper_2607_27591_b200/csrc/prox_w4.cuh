@@ -519,33 +519,41 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) 
         z0 = zr[e0];
         z1 = zr[8 * St::kZeros + e1];
       }
+      int d[NT][4];                                            // 16 times the group's sums
+      float2 off[NT];
 #pragma unroll
       for (int m = 0; m < NT; ++m) {
-        int d[4] = {0, 0, 0, 0};                               // 16 times the group's sums
-        float2 off = make_float2(0.f, 0.f);
         const int at = ((c - cb0) * (4 / W) + j) * cols + m * 8 + 2 * t;
         if (ZP) {
-          off = *reinterpret_cast<const float2*>(sx + at);
+          off[m] = *reinterpret_cast<const float2*>(sx + at);
+          d[m][0] = d[m][1] = d[m][2] = d[m][3] = 0;
         } else {
           const int4 v = *reinterpret_cast<const int4*>(sx + at * 2);
-          d[0] = v.x; d[1] = v.y; d[2] = v.z; d[3] = v.w;
-        }
-#pragma unroll
-        for (int p = 0; p < (W + 1) / 2; ++p) {
-          const uint4 v = xc[((j * W + 2 * p) >> 1) * cols * 4 + m * 32];   // low columns of two words, high columns
-          if (W > 1) {
-            mma(d, d, lw[p][0], lw[p][1], lw[p][2], lw[p][3], v.x, v.y);
-            mma(d, d, hw[p][0], hw[p][1], hw[p][2], hw[p][3], v.z, v.w);
-          } else {
-            mma(d, d, lw[p][0], lw[p][1], hw[p][0], hw[p][1], j & 1 ? v.y : v.x, j & 1 ? v.w : v.z);
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float v = ZP ? fmaf(e < 2 ? -z0 : -z1, e & 1 ? off.y : off.x, (float)d[e]) : (float)d[e];
-          acc[m][e] = fmaf(e < 2 ? f0 : f1, v, acc[m][e]);
+          d[m][0] = v.x; d[m][1] = v.y; d[m][2] = v.z; d[m][3] = v.w;
         }
       }
+#pragma unroll
+      for (int p = 0; p < (W + 1) / 2; ++p) {                  // (steps that follow one another are of different sums)
+        uint4 v[NT];                                           // low columns of two words, high columns
+#pragma unroll
+        for (int m = 0; m < NT; ++m) v[m] = xc[((j * W + 2 * p) >> 1) * cols * 4 + m * 32];
+#pragma unroll
+        for (int m = 0; m < NT; ++m) {
+          if (W > 1) mma(d[m], d[m], lw[p][0], lw[p][1], lw[p][2], lw[p][3], v[m].x, v[m].y);
+          else mma(d[m], d[m], lw[p][0], lw[p][1], hw[p][0], hw[p][1], j & 1 ? v[m].y : v[m].x, j & 1 ? v[m].w : v[m].z);
+        }
+        if (W > 1) {
+#pragma unroll
+          for (int m = 0; m < NT; ++m) mma(d[m], d[m], hw[p][0], hw[p][1], hw[p][2], hw[p][3], v[m].z, v[m].w);
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float v = ZP ? fmaf(e < 2 ? -z0 : -z1, e & 1 ? off[m].y : off[m].x, (float)d[m][e]) : (float)d[m][e];
+          acc[m][e] = fmaf(e < 2 ? f0 : f1, v, acc[m][e]);
+        }
     }
   };
   // one output of unit u: row r of its WM * 16 tile rows (linear), or channel r of its WM * 8 (gate and up)
