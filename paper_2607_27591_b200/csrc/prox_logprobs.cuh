@@ -9,10 +9,10 @@
 // room for; its blocks' sums and lists meet in shared memory of the first block, in their order.
 //
 // Top alternatives.  Order: by value, then the lower index; as one 64-bit key, value bits made monotonic above, inverted
-// index below.  A block takes rounds of up to 16 vectors a thread.  A thread's largest value of the round is known from the
-// softmax; in the first round the k-th largest of 64 values of groups of threads is a floor that k logits reach, from
-// then on the k-th largest of the candidates kept is one.  Only what reaches the floor is stored.  If that is more than the list
-// holds, exact steps follow (settle).
+// index below.  A block takes rounds of 4 vectors a thread.  The vectors' maxima are known from the softmax; in the first round
+// the k-th largest of the maxima of 64 groups of threads is a floor that k logits reach, so only vectors that reach it are noted,
+// by their number.  Noted vectors are looked at all together (process): their logits above the floor go to a list, and behind the
+// first round, and whenever the list fills up, the k-th largest in it is the new floor (settle).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -29,7 +29,8 @@ constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxTop = 32;
 constexpr int kVectors = 4;              // 16-byte vectors of a thread and round
-constexpr int kList = 2048;              // candidates of a block
+constexpr int kList = 2 * kThreads;      // candidates of a block
+constexpr int kItems = 2 * kVectors * kThreads;   // vectors noted
 constexpr int kMaxCluster = 8;
 
 struct Args {
@@ -86,6 +87,8 @@ __device__ __forceinline__ float value_of(unsigned long long key) {
   return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
 }
 __device__ __forceinline__ int index_of(unsigned long long key) { return (int)~(uint32_t)key; }
+// The largest key below all of value v (which is a number).
+__device__ __forceinline__ unsigned long long key_below(float v) { return (key_of(v, 0) & ~0xffffffffull) - 1; }
 
 // Running softmax sums: m in logits, d = (x - m) log2 e / temperature, s = sum 2^d, w = sum d 2^d.
 struct Sums { float m, s, w; };
@@ -153,9 +156,10 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
   constexpr int kPer = Type<DT>::kPer, kSize = Type<DT>::kSize;
   __shared__ Sums warp_sums[kWarps];
   __shared__ Sums block_sums;
-  __shared__ unsigned long long list[TOP ? kList : 1], best[TOP ? kMaxTop : 1];
+  __shared__ unsigned long long list[TOP ? kList : 1], tops[TOP ? kThreads : 1], best[TOP ? kMaxTop : 1];
+  __shared__ unsigned long long floor_key;                     // only keys above it count
+  __shared__ int items[TOP ? kItems : 1], n_items;
   __shared__ float group_max[64];
-  __shared__ float floor_now;
   __shared__ int count;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int S = a.S, rank = blockIdx.x % S;
@@ -190,7 +194,7 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
   };
 
   if (TOP) {
-    if (tid == 0) { count = 0; floor_now = __uint_as_float(0xff800000u); }
+    if (tid == 0) { count = 0; n_items = 0; floor_key = 0; }
   }
   // The k largest of the list's first n keys, in order, to its front; raises the floor.  All threads; n <= kList.
   auto settle = [&](int n) {
@@ -209,34 +213,49 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
     if (tid < min(n, a.k)) list[tid] = best[tid];
     if (tid == 0) {
       count = min(n, a.k);
-      if (n >= a.k) floor_now = value_of(best[a.k - 1]);
+      if (n >= a.k) floor_key = max(floor_key, best[a.k - 1]);
     }
     __syncthreads();
   };
-  auto each = [&](const uint4 (&v)[kVectors], int q, float floor_v, auto&& f) {   // a thread's logits of a round that reach the floor
-#pragma unroll
-    for (int j = 0; j < kVectors; ++j) {
-      float x[kPer], most = __uint_as_float(0xff800000u);
-      widen<DT>(x, v[j]);
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) most = max_nan(most, x[e]);
-      if (most < floor_v || q + j * kThreads >= q1) continue;
-      const int first = (q + j * kThreads) * kPer - head;
-#pragma unroll
-      for (int e = 0; e < kPer; ++e)
-        if (!(x[e] < floor_v) && first + e >= 0 && first + e < a.V) f(x[e], first + e);
-    }
+  auto key_at = [&](int item, int e) -> unsigned long long {   // of a noted vector's logit e; 0 if it is none
+    const int index = items[item] * kPer + e - head;
+    if (index < 0 || index >= a.V) return 0;
+    return key_of(widen<DT>(reinterpret_cast<const T*>(start)[index]), index);
   };
-  auto each_again = [&](int q, auto&& f) {                     // the same, read once more: short code for what happens seldom
+  // Looks at the n noted vectors.  All threads, behind a barrier; leaves none.
+  auto process = [&](int n) {
+    if (n > kThreads / 2) {
+      // so many (rising or equal logits): the k-th largest of the threads' largest keys is a floor too
+      unsigned long long top = 0;
 #pragma unroll 1
-    for (int j = 0; j < kVectors; ++j) {
-      const uint4 v = load(q + j * kThreads);
-      const T* x = reinterpret_cast<const T*>(&v);
-      for (int e = 0; e < kPer; ++e) {
-        const int index = (q + j * kThreads) * kPer + e - head;
-        if (q + j * kThreads < q1 && index >= 0 && index < a.V) f(widen<DT>(x[e]), index);
-      }
+      for (int i = tid; i < n; i += kThreads)
+        for (int e = 0; e < kPer; ++e) top = max(top, key_at(i, e));
+      tops[tid] = top;
+      if (tid == 0) best[0] = 0;
+      __syncthreads();
+      int above = 0;
+#pragma unroll 8
+      for (int j = 0; j < kThreads; ++j) above += tops[j] > top;
+      if (above == a.k - 1 && top) best[0] = top;              // (keys differ; threads without a logit have 0)
+      __syncthreads();
+      if (tid == 0 && best[0]) floor_key = max(floor_key, best[0] - 1);
+      __syncthreads();
     }
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += kThreads / kPer) {
+      const int i = i0 + tid / kPer;
+      int end = 0;
+      if (i < n) {
+        const unsigned long long key = key_at(i, tid % kPer);
+        if (key > floor_key) {
+          end = atomicAdd(&count, 1) + 1;
+          list[end - 1] = key;
+        }
+      }
+      if (__syncthreads_or(end > kList / 2)) settle(count);    // (at most kThreads more)
+    }
+    if (tid == 0) n_items = 0;
+    __syncthreads();
   };
 
   Sums sum = {-3.402823466e38f, 0.f, 0.f};
@@ -269,14 +288,18 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
       for (int j = 0; j < kVectors; ++j) next[j] = load(q + (kVectors + j) * kThreads);
     }
     ahead += kVectors * kThreads * 16;
-    float most = __uint_as_float(0xff800000u);
+    float vector_max[kVectors];
 #pragma unroll
     for (int j = 0; j < kVectors; ++j) {
       float x[kPer];
       widen<DT>(x, now[j]);
+      vector_max[j] = x[0];
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) most = max_nan(most, x[e]);
+      for (int e = 1; e < kPer; ++e) vector_max[j] = max_nan(vector_max[j], x[e]);
     }
+    float most = vector_max[0];
+#pragma unroll
+    for (int j = 1; j < kVectors; ++j) most = max_nan(most, vector_max[j]);
     if (!(most <= sum.m)) raise(sum, most, c);
     {
       uint64_t s2 = pair(0.f, 0.f), w2 = s2;
@@ -303,6 +326,7 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
       sum.w += w0 + w1;
     }
     if (TOP) {
+      const bool start_floor = first_round;
       if (first_round) {
         // a floor that at least k logits reach: the k-th largest of the maxima of 64 groups of eight threads
         first_round = false;
@@ -321,58 +345,22 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
         }
 #pragma unroll
         for (int o = 1; o < 8; o <<= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
-        if ((tid & 7) == 0 && above == a.k - 1 && mine == mine) floor_now = mine;
+        if ((tid & 7) == 0 && above == a.k - 1 && mine == mine) floor_key = key_below(mine);
         __syncthreads();
       }
-      const float floor_v = floor_now;
+      const float floor_v = value_of(floor_key + 1);           // (of a key below all of a value: that value; 0: the lowest)
       int end = 0;
       if (!(most < floor_v)) {
-        each(now, q, floor_v, [&](float x, int index) {
-          end = atomicAdd(&count, 1) + 1;
-          if (end <= kList) list[end - 1] = key_of(x, index);
-        });
-      }
-      if (__syncthreads_or(end > kList / 2)) {
-        int n = count;
-        __syncthreads();
-        if (n > kList) {
-          // More than the list holds, in this round (before it there were at most half as many): take this round's additions
-          // back, find the k-th largest of the threads' largest keys, and store what reaches it: k threads' logits at most
-          if (tid == 0) count = 0;
-          __syncthreads();
-          for (int i = tid; i < kList; i += kThreads) {
-            const int index = index_of(list[i]), v = (index + head) / kPer;
-            if (v >= qr && v < qr + kVectors * kThreads) list[i] = 0;
+#pragma unroll
+        for (int j = 0; j < kVectors; ++j)
+          if (!(vector_max[j] < floor_v) && q + j * kThreads < q1) {
+            end = atomicAdd(&n_items, 1) + 1;
+            items[end - 1] = q + j * kThreads;
           }
-          __syncthreads();
-          // what is left of earlier rounds, moved together (at most half the list)
-          unsigned long long kept[kList / kThreads];
-#pragma unroll
-          for (int i = 0; i < kList / kThreads; ++i) kept[i] = list[tid + i * kThreads];
-          __syncthreads();
-#pragma unroll
-          for (int i = 0; i < kList / kThreads; ++i)
-            if (kept[i]) list[atomicAdd(&count, 1)] = kept[i];
-          unsigned long long top = 0;
-          each_again(q, [&](float x, int index) { top = max(top, key_of(x, index)); });
-          __syncthreads();
-          list[kList - kThreads + tid] = top;
-          __syncthreads();
-          int above = 0;
-          for (int j = 0; j < kThreads; ++j) above += list[kList - kThreads + j] > top;
-          if (above == a.k - 1) best[0] = top;                 // (keys differ; threads without a logit have 0 and are last)
-          __syncthreads();
-          const unsigned long long least = best[0];
-          __syncthreads();
-          if (top >= least)
-            each_again(q, [&](float x, int index) {
-              const unsigned long long key = key_of(x, index);
-              if (key >= least) list[atomicAdd(&count, 1)] = key;
-            });
-          __syncthreads();
-          n = count;
-        }
-        settle(n);
+      }
+      if (__syncthreads_or(end > kItems / 2) || (start_floor && more)) {
+        process(n_items);
+        if (start_floor) settle(count);                        // the k-th largest of the first round: later ones bring few above it
       }
     }
 #pragma unroll
@@ -387,7 +375,10 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
   }
   if (lane == 0) warp_sums[warp] = sum;
   __syncthreads();
-  if (TOP) settle(count);
+  if (TOP) {
+    process(n_items);
+    settle(count);
+  }
   // of as many sums as there are (a power of two), one a lane of the first warp: joined in pairs
   auto join_lanes = [&](Sums v, int n) {
     for (int o = 1; o < n; o <<= 1) {
