@@ -150,17 +150,90 @@ __device__ __forceinline__ uint32_t cluster_address(const void* p, int rank) {
 }
 __device__ __forceinline__ void cluster_barrier() { asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory"); }
 
+// What a block keeps for the top alternatives.
+template <bool TOP>
+struct Top {
+  unsigned long long list[TOP ? kList : 1], tops[TOP ? kThreads : 1], best[TOP ? kMaxTop : 1];
+  unsigned long long floor_key;          // only keys above it count
+  int items[TOP ? kItems : 1], n_items, count;
+};
+
+// The k largest of the list's first n keys, in order, to its front; raises the floor.  All threads; n <= kList.  (Not inlined, as
+// process: what is rare is kept from the registers of the loop around it.)
+__device__ __noinline__ void settle(Top<true>& s, int n, int k) {
+  const int tid = threadIdx.x, parts = n <= kThreads / 4 ? 4 : n <= kThreads / 2 ? 2 : 1;
+  for (int i0 = 0; i0 < n; i0 += kThreads / parts) {
+    const int i = i0 + tid / parts;
+    const unsigned long long mine = i < n ? s.list[i] : ~0ull;
+    int above = 0;
+#pragma unroll 8
+    for (int j = tid % parts; j < n; j += parts) above += s.list[j] > mine;
+    if (parts > 1) above += __shfl_xor_sync(0xffffffffu, above, 1);
+    if (parts > 2) above += __shfl_xor_sync(0xffffffffu, above, 2);
+    if (i < n && tid % parts == 0 && above < k) s.best[above] = mine;
+  }
+  __syncthreads();
+  if (tid < min(n, k)) s.list[tid] = s.best[tid];
+  if (tid == 0) {
+    s.count = min(n, k);
+    if (n >= k) s.floor_key = max(s.floor_key, s.best[k - 1]);
+  }
+  __syncthreads();
+}
+
+// Looks at the n noted vectors of a row.  All threads, behind a barrier; leaves none.
+template <int DT>
+__device__ __noinline__ void process(Top<true>& s, int n, int k, const uint8_t* start, int head, int V) {
+  using T = typename Type<DT>::T;
+  constexpr int kPer = Type<DT>::kPer;
+  const int tid = threadIdx.x;
+  auto key_at = [&](int item, int e) -> unsigned long long {   // of a noted vector's logit e; 0 if it is none
+    const int index = s.items[item] * kPer + e - head;
+    if (index < 0 || index >= V) return 0;
+    return key_of(widen<DT>(reinterpret_cast<const T*>(start)[index]), index);
+  };
+  if (n > kThreads / 2) {
+    // so many (rising or equal logits): the k-th largest of the threads' largest keys is a floor too
+    unsigned long long most = 0;
+#pragma unroll 1
+    for (int i = tid; i < n; i += kThreads)
+      for (int e = 0; e < kPer; ++e) most = max(most, key_at(i, e));
+    s.tops[tid] = most;
+    if (tid == 0) s.best[0] = 0;
+    __syncthreads();
+    int above = 0;
+#pragma unroll 8
+    for (int j = 0; j < kThreads; ++j) above += s.tops[j] > most;
+    if (above == k - 1 && most) s.best[0] = most;              // (keys differ; threads without a logit have 0)
+    __syncthreads();
+    if (tid == 0 && s.best[0]) s.floor_key = max(s.floor_key, s.best[0] - 1);
+    __syncthreads();
+  }
+#pragma unroll 1
+  for (int i0 = 0; i0 < n; i0 += kThreads / kPer) {
+    const int i = i0 + tid / kPer;
+    int end = 0;
+    if (i < n) {
+      const unsigned long long key = key_at(i, tid % kPer);
+      if (key > s.floor_key) {
+        end = atomicAdd(&s.count, 1) + 1;
+        s.list[end - 1] = key;
+      }
+    }
+    if (__syncthreads_or(end > kList / 2)) settle(s, s.count, k);   // (at most kThreads more)
+  }
+  if (tid == 0) s.n_items = 0;
+  __syncthreads();
+}
+
 template <int DT, bool TOP>
 __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
   using T = typename Type<DT>::T;
   constexpr int kPer = Type<DT>::kPer, kSize = Type<DT>::kSize;
   __shared__ Sums warp_sums[kWarps];
   __shared__ Sums block_sums;
-  __shared__ unsigned long long list[TOP ? kList : 1], tops[TOP ? kThreads : 1], best[TOP ? kMaxTop : 1];
-  __shared__ unsigned long long floor_key;                     // only keys above it count
-  __shared__ int items[TOP ? kItems : 1], n_items;
+  __shared__ Top<TOP> top;
   __shared__ float group_max[64];
-  __shared__ int count;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int S = a.S, rank = blockIdx.x % S;
   const long long row = blockIdx.x / S;
@@ -194,70 +267,8 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
   };
 
   if (TOP) {
-    if (tid == 0) { count = 0; n_items = 0; floor_key = 0; }
+    if (tid == 0) { top.count = 0; top.n_items = 0; top.floor_key = 0; }
   }
-  // The k largest of the list's first n keys, in order, to its front; raises the floor.  All threads; n <= kList.
-  auto settle = [&](int n) {
-    const int parts = n <= kThreads / 4 ? 4 : n <= kThreads / 2 ? 2 : 1;
-    for (int i0 = 0; i0 < n; i0 += kThreads / parts) {
-      const int i = i0 + tid / parts;
-      const unsigned long long mine = i < n ? list[i] : ~0ull;
-      int above = 0;
-#pragma unroll 8
-      for (int j = tid % parts; j < n; j += parts) above += list[j] > mine;
-      if (parts > 1) above += __shfl_xor_sync(0xffffffffu, above, 1);
-      if (parts > 2) above += __shfl_xor_sync(0xffffffffu, above, 2);
-      if (i < n && tid % parts == 0 && above < a.k) best[above] = mine;
-    }
-    __syncthreads();
-    if (tid < min(n, a.k)) list[tid] = best[tid];
-    if (tid == 0) {
-      count = min(n, a.k);
-      if (n >= a.k) floor_key = max(floor_key, best[a.k - 1]);
-    }
-    __syncthreads();
-  };
-  auto key_at = [&](int item, int e) -> unsigned long long {   // of a noted vector's logit e; 0 if it is none
-    const int index = items[item] * kPer + e - head;
-    if (index < 0 || index >= a.V) return 0;
-    return key_of(widen<DT>(reinterpret_cast<const T*>(start)[index]), index);
-  };
-  // Looks at the n noted vectors.  All threads, behind a barrier; leaves none.
-  auto process = [&](int n) {
-    if (n > kThreads / 2) {
-      // so many (rising or equal logits): the k-th largest of the threads' largest keys is a floor too
-      unsigned long long top = 0;
-#pragma unroll 1
-      for (int i = tid; i < n; i += kThreads)
-        for (int e = 0; e < kPer; ++e) top = max(top, key_at(i, e));
-      tops[tid] = top;
-      if (tid == 0) best[0] = 0;
-      __syncthreads();
-      int above = 0;
-#pragma unroll 8
-      for (int j = 0; j < kThreads; ++j) above += tops[j] > top;
-      if (above == a.k - 1 && top) best[0] = top;              // (keys differ; threads without a logit have 0)
-      __syncthreads();
-      if (tid == 0 && best[0]) floor_key = max(floor_key, best[0] - 1);
-      __syncthreads();
-    }
-#pragma unroll 1
-    for (int i0 = 0; i0 < n; i0 += kThreads / kPer) {
-      const int i = i0 + tid / kPer;
-      int end = 0;
-      if (i < n) {
-        const unsigned long long key = key_at(i, tid % kPer);
-        if (key > floor_key) {
-          end = atomicAdd(&count, 1) + 1;
-          list[end - 1] = key;
-        }
-      }
-      if (__syncthreads_or(end > kList / 2)) settle(count);    // (at most kThreads more)
-    }
-    if (tid == 0) n_items = 0;
-    __syncthreads();
-  };
-
   Sums sum = {-3.402823466e38f, 0.f, 0.f};
   uint4 now[kVectors], next[kVectors];
 #pragma unroll
@@ -325,7 +336,7 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
       sum.s += s0 + s1;
       sum.w += w0 + w1;
     }
-    if (TOP) {
+    if constexpr (TOP) {
       const bool start_floor = first_round;
       if (first_round) {
         // a floor that at least k logits reach: the k-th largest of the maxima of 64 groups of eight threads
@@ -345,22 +356,22 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
         }
 #pragma unroll
         for (int o = 1; o < 8; o <<= 1) above += __shfl_xor_sync(0xffffffffu, above, o);
-        if ((tid & 7) == 0 && above == a.k - 1 && mine == mine) floor_key = key_below(mine);
+        if ((tid & 7) == 0 && above == a.k - 1 && mine == mine) top.floor_key = key_below(mine);
         __syncthreads();
       }
-      const float floor_v = value_of(floor_key + 1);           // (of a key below all of a value: that value; 0: the lowest)
+      const float floor_v = value_of(top.floor_key + 1);           // (of a key below all of a value: that value; 0: the lowest)
       int end = 0;
       if (!(most < floor_v)) {
 #pragma unroll
         for (int j = 0; j < kVectors; ++j)
           if (!(vector_max[j] < floor_v) && q + j * kThreads < q1) {
-            end = atomicAdd(&n_items, 1) + 1;
-            items[end - 1] = q + j * kThreads;
+            end = atomicAdd(&top.n_items, 1) + 1;
+            top.items[end - 1] = q + j * kThreads;
           }
       }
       if (__syncthreads_or(end > kItems / 2) || (start_floor && more)) {
-        process(n_items);
-        if (start_floor) settle(count);                        // the k-th largest of the first round: later ones bring few above it
+        process<DT>(top, top.n_items, a.k, start, head, a.V);
+        if (start_floor) settle(top, top.count, a.k);                        // the k-th largest of the first round: later ones bring few above it
       }
     }
 #pragma unroll
@@ -375,9 +386,9 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
   }
   if (lane == 0) warp_sums[warp] = sum;
   __syncthreads();
-  if (TOP) {
-    process(n_items);
-    settle(count);
+  if constexpr (TOP) {
+    process<DT>(top, top.n_items, a.k, start, head, a.V);
+    settle(top, top.count, a.k);
   }
   // of as many sums as there are (a power of two), one a lane of the first warp: joined in pairs
   auto join_lanes = [&](Sums v, int n) {
@@ -403,25 +414,23 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
         v = join_lanes(v, S);
         if (lane == 0) warp_sums[0] = v;
       }
-      if (TOP) {
+      if constexpr (TOP) {
         for (int i = tid; i < (S - 1) * a.k; i += kThreads) {  // (a block may have had fewer logits than k)
           const int r = i / a.k + 1, j = i - (r - 1) * a.k;
           int n;
           unsigned long long key;
-          asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(n) : "r"(cluster_address(&count, r)) : "memory");
-          asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(key) : "r"(cluster_address(&list[j], r)) : "memory");
-          if (j < n) list[kMaxTop + i] = key;
-          else list[kMaxTop + i] = 0;
+          asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(n) : "r"(cluster_address(&top.count, r)) : "memory");
+          asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(key) : "r"(cluster_address(&top.list[j], r)) : "memory");
+          top.list[kMaxTop + i] = j < n ? key : 0;
         }
       }
     }
     cluster_barrier();                                         // nobody leaves while its memory is read
     if (rank != 0) return;
-    if (TOP) {
-      if (tid >= count && tid < kMaxTop) list[tid] = 0;
-      if (tid >= a.k && tid < kMaxTop) list[tid] = 0;
+    if constexpr (TOP) {
+      if (tid >= top.count && tid < kMaxTop) top.list[tid] = 0;   // (it has k at most)
       __syncthreads();
-      settle(kMaxTop + (S - 1) * a.k);
+      settle(top, kMaxTop + (S - 1) * a.k, a.k);
     }
     if (tid == 0) block_sums = warp_sums[0];
   }
@@ -442,8 +451,8 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
     a.logprob[row * a.n_given + i] = given < 0 ? 0.f : given >= a.V ? __uint_as_float(0x7fffffffu) : log_p(given_logit);
   }
   if (TOP && tid < a.k) {
-    a.top_logprob[row * a.k + tid] = log_p(value_of(list[tid]));
-    a.top_index[row * a.k + tid] = index_of(list[tid]);
+    a.top_logprob[row * a.k + tid] = log_p(value_of(top.list[tid]));
+    a.top_index[row * a.k + tid] = index_of(top.list[tid]);
   }
 }
 
