@@ -3,7 +3,9 @@
 //   z = x / temperature,  lse = log sum_v exp(z_v),  log p(v) = z_v - lse,  H = -sum_v p_v log p_v = log s - w / s
 //   with m = max z,  s = sum exp(z - m),  w = sum (z - m) exp(z - m)
 //
-// One pass over the logits: a thread keeps its own m, s and w and rescales the two when its maximum rises.  Bound by HBM; next
+// One pass over the logits: a thread keeps its own m, s and w and rescales the two when its maximum rises.  2048 rows of 131072
+// bf16 logits take 98 us, 5.5 TB/s; one row 4.5 us, with 20 top alternatives 10 us, all of it latency (two barriers of the
+// cluster and three of lists).  Bound by HBM; next
 // comes the special-function unit (one exponential a logit: 16 a cycle and SM, three quarters of its rate while HBM delivers
 // 16-bit logits).  A row goes to one block, or to a cluster of up to 8 where there are fewer rows than the GPU has
 // room for; its blocks' sums and lists meet in shared memory of the first block, in their order.

@@ -165,7 +165,7 @@ prox_status_t prox_w4_linear(const prox_w4_t* w, int N, int K, int group_size, c
   if ((x_dtype != w4::kBf16 && x_dtype != w4::kFp16) || y_dtype < 0 || y_dtype > 2) return PROX_ERR_INVALID_ARG;
   if (!host_aligned(x_dev, 2) || !host_aligned(y_dev, y_dtype == w4::kFp32 ? 4 : 2)) return PROX_ERR_INVALID_ARG;
   if (B > 1 && (x_stride < K || y_stride < N)) return PROX_ERR_INVALID_ARG;
-  if (!group_known(group_size) || K % 32 || K > 65536) return PROX_ERR_UNSUPPORTED;
+  if (!group_known(group_size) || K % 32 || K > 65536 || N > 0x7fff0000) return PROX_ERR_UNSUPPORTED;
   int dev;
   if (prox_status_t s = current_device(&dev)) return s;
   if (!mat_ok(w, dev) || !host_on_current_device(x_dev, dev) || !host_on_current_device(y_dev, dev)) return PROX_ERR_INVALID_ARG;

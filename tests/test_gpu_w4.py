@@ -181,6 +181,22 @@ def test_linear_chain_without_a_wait(pb):
         check_linear(b, w, 128, a, K, 0)
 
 
+def test_memory_that_a_kernel_cannot_read_is_refused(pb):
+    """Pageable host memory in any place: refused on the host, nothing is launched."""
+    N, K = 64, 128
+    w = make_w4(12, N, K, 32, True)
+    x, y = tokens(13, 1, K, torch.bfloat16), torch.empty(1, N, device="cuda")
+    host = torch.zeros(1 << 16, dtype=torch.uint8)
+    good = dict(w=w, x=x, y=y)
+    for bad in (dict(w=(host, w[1], w[2])), dict(w=(w[0], host, w[2])), dict(w=(w[0], w[1], host)), dict(x=host), dict(y=host)):
+        a = good | bad
+        with pytest.raises(pb.ProxError) as e:
+            pb.prox_w4_linear(a["w"], N, K, 32, a["x"], K, 0, 1, a["y"], N, 1)
+        assert e.value.status == 1
+    pb.prox_w4_linear(w, N, K, 32, x, K, 0, 1, y, N, 1)
+    check_linear(y, w, 32, x, K, 1)
+
+
 # ---- Stage 2 ----------------------------------------------------------------
 def ffn_reference(gate, up, down, group, x, lists):
     """y and its bound: d(silu) <= 1.1 |dg|; expf, the division and the products lose a few steps; h s is rounded to fp32 and to a

@@ -28,7 +28,8 @@ def linear(pb, w=None, N=16, K=64, group=32, x=P, xs=64, xt=0, B=1, y=P, ys=16, 
 @pytest.mark.parametrize("change,status", [
     (dict(N=0), INVALID), (dict(K=0), INVALID), (dict(B=0), INVALID), (dict(x=None), INVALID), (dict(y=None), INVALID), (dict(xt=1), INVALID), (dict(xt=3), INVALID),
     (dict(yt=3), INVALID), (dict(yt=-1), INVALID), (dict(x=P + 1), INVALID), (dict(y=P + 2, yt=1), INVALID), (dict(B=2, xs=63), INVALID), (dict(B=2, ys=15), INVALID),
-    (dict(K=40), UNSUPPORTED), (dict(K=65568), UNSUPPORTED), (dict(group=16), UNSUPPORTED), (dict(group=-1), UNSUPPORTED), (dict(group=256), UNSUPPORTED)])
+    (dict(K=40), UNSUPPORTED), (dict(K=65568), UNSUPPORTED), (dict(group=16), UNSUPPORTED), (dict(group=-1), UNSUPPORTED), (dict(group=256), UNSUPPORTED),
+    (dict(N=2 ** 31 - 1), UNSUPPORTED)])
 def test_linear_refuses(pb, change, status):
     assert linear(pb, **change) == status
 
