@@ -35,7 +35,7 @@ int clusters_at_once(int device, int S, int threads, size_t smem) {
 }
 
 // The shape that is done first, in cycles: an SM takes about 48 for 128 columns of a tile when all its warps are busy (18
-// more for every 8 further columns of digits), a warp alone 300 (100 more); the end of a unit costs 1500, much less where no warp waits for
+// more for every 8 further columns of digits), a warp alone 400 (150 more); the end of a unit costs 1500, much less where no warp waits for
 // another, the cluster's sum 5000; a token's digits are made at 4 inputs a cycle.
 RowsPlan plan_rows(int tiles, int K, int B, int words, int nt, int sms, int dev) {
   const int C = (K + 127) / 128;
@@ -52,9 +52,9 @@ RowsPlan plan_rows(int tiles, int K, int B, int words, int nt, int sms, int dev)
           const size_t fixed = w4::rows_fixed_bytes(Cs, nt, words) + (WK > 1 ? w4::rows_red_bytes(nt) : 0) +
                                (size_t)w4::kRowWarps * stages * w4::rows_stage_bytes(words);
           if (fixed + sum > (size_t)kMaxSmem) continue;
-          const int units = (tiles + WM - 1) / WM, clusters = std::max(1, std::min(units, at_once)), mine = (units + clusters - 1) / clusters;
+          const int clusters = std::max(1, std::min(tiles, at_once)), most = (tiles + clusters - 1) / clusters, mine = (most + WM - 1) / WM;
           const int R = S > 1 ? (int)std::min<size_t>(std::min(mine, 16), (kMaxSmem - fixed) / sum) : 0;
-          const double cost = (double)mine * std::max(WM * Cs * (30 + 18 * nt), w4::rows_run(Cs, WK) * (200 + 100 * nt)) * (1.0 + 0.3 / stages) +
+          const double cost = std::max((double)most * Cs * (30 + 18 * nt), (double)mine * w4::rows_run(Cs, WK) * (250 + 150 * nt)) * (1.0 + 0.3 / stages) +
                               mine * (WK == 1 ? 300.0 : 1500.0) + (S > 1 ? 5000.0 * ((mine + R - 1) / R) : 0.0) + Cs * 32.0 * B;
           if (cost < least - 1e-9) {
             least = cost;

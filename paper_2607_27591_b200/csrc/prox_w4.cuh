@@ -256,7 +256,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) 
   constexpr int kPer = GATEUP ? 8 : 16;                        // list entries of a tile
   const int wm = warp / WK, wk = warp - wm * WK;
   int id_next = -1, bits_next = 1;                             // GATEUP: a channel and its tokens' bits, as they are in the lists
-  auto entry = [&](int u) { return ((cid + u * ncl) * WM + wm) * kPer + g; };   // list entry of this lane's first row
+  // tile of a unit's warps i: the clusters take turns, so that what is left in the last unit is spread over all of them
+  auto tile_of = [&](int u, int i) { return (u * WM + i) * ncl + cid; };
+  auto entry = [&](int u) { return tile_of(u, wm) * kPer + g; };   // list entry of this lane's first row
   auto fetch_id = [&](int u) {                                 // asked for one unit ahead of its rows, and not looked at before
     if (GATEUP && a.n > 0) {
       const int pos = min(entry(u), a.n - 1);                  // (an entry behind the list's end is not used)
@@ -270,12 +272,13 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) 
     n = a.n;
     if (a.count) n = max(0, min(n, *a.count));
   }
-  const int U = (n + kPer * WM - 1) / (kPer * WM);
-  if (cid >= U) {                                              // the whole cluster
+  const int tiles = (n + kPer - 1) / kPer;
+  if (cid >= tiles) {                                          // the whole cluster
     if (GATEUP && tid < B) a.hmax[blockIdx.x * B + tid] = 0;
     return;
   }
-  const int nu = (U - cid - 1) / ncl + 1;
+  const int nu = (tiles + ncl * WM - 1) / (ncl * WM);          // units of the cluster
+  const int mine = wm < WM && tile_of(0, wm) < tiles ? (tiles - 1 - tile_of(0, wm)) / (ncl * WM) + 1 : 0;   // those in which this warp has a tile
 
   const int cw = rows_run(Cs, WK), nb = cw / kBatch;           // chunks and batches of a warp and unit (the last warps may have fewer)
   const int c0 = cb0 + wk * cw, c1 = wm < WM ? min(cb1, c0 + cw) : c0;
@@ -296,7 +299,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) 
       const bool known = (unsigned)id_next < (unsigned)a.rows;
       r0 = r1 = known ? id_next : 0;
       if (wk == 0 && t == 0) sid[lu & 7][wm * 8 + g] = known ? bits_next : 0;
-      if (lu + 1 < nu) fetch_id(lu + 1);
+      if (lu + 1 < mine) fetch_id(lu + 1);
     } else {
       r0 = min(entry(lu), a.rows - 1);
       r1 = min(entry(lu) + 8, a.rows - 1);
@@ -344,7 +347,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) 
   };
   const int whole_batches = max(0, min(c1, a.K / 128) - c0) / kBatch;   // batches of a unit that are inside the row
   auto issue = [&]() {                                         // the next batch; nothing behind the last one
-    if (lu < nu) {
+    if (lu < mine) {
       const uint32_t to = stages_at + lslot * St::kBytes;
       const int at = lb * (kBatch * 64);
       if (aligned && lb < whole_batches) {
@@ -366,7 +369,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) 
       if (++lslot == a.stages) lslot = 0;
       if (++lb == nb) {
         lb = 0;
-        if (++lu < nu) open_unit();
+        if (++lu < mine) open_unit();
       }
     }
     copies_end();
@@ -426,7 +429,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) 
         if (lane == 0 && m) atomicMax(xmax + b, bits);
       }
     }
-    if (wm < WM) {                                             // the first weights: on their way meanwhile
+    if (mine > 0) {                                            // the first weights: on their way meanwhile
       open_unit();
 #pragma unroll 1
       for (int d = 0; d < a.stages; ++d) issue();
@@ -564,7 +567,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) 
   };
   // one output of unit u: row r of its WM * 16 tile rows (linear), or channel r of its WM * 8 (gate and up)
   auto emit = [&](int u, int r, int b, float v, float up) {
-    const int pos = (cid + u * ncl) * WM * kPer + r;
+    const int pos = tile_of(u, r / kPer) * kPer + r % kPer;
     if (pos >= n) return;
     if (!GATEUP) {
       store(a.y, (size_t)b * a.y_stride + pos, v, a.y_type);
@@ -654,7 +657,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_kernel(const RowsArgs a) 
   int slot = 0;
 #pragma unroll 1
   for (int u = 0; u < nu; ++u) {
-    if (wm < WM) {                                             // (others have no tile of their own)
+    if (u < mine) {                                            // (else the warp has no tile in this unit)
       int e0 = shifts[warp][u & 7][g], e1 = shifts[warp][u & 7][8 + g];
 #pragma unroll 1
       for (int batch = 0; batch < nb; ++batch) {
