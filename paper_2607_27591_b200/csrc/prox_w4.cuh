@@ -157,15 +157,15 @@ __device__ __forceinline__ void cluster_barrier() {
 // A warp owns tiles of 16 rows (linear) or of 8 channels (rows 0-7 of the tile are gate rows, rows 8-15 the up rows of
 // the same channels, so that both pre-activations of a channel end in one place) and a run of 128-column chunks; it copies two
 // chunks of its 16 rows at a time, a 128-byte line each, to a ring of its own in shared memory (plain loads of a lane's share, 64
-// bytes of a row at a time, were waited for: 70 us against 54 for 131072 x 4096 and one token).  A block has WM tiles side by
+// bytes of a row at a time, were waited for: 70 us against 57 for 131072 x 4096 and one token).  A block has WM tiles side by
 // side and WK warps along the columns of each; a cluster of S blocks splits the columns further where the rows alone do not
 // fill the GPU or the tokens do not fit in shared memory.  With one warp along the columns nothing is shared and warps run on
 // their own; else partial sums meet in shared memory, of the cluster where it has more than one block, in a fixed order: results
 // do not depend on timing.
 //
-// Measured in a chain of calls, weights from HBM (6.57 TB/s copied): one token, 131072 x 4096 with groups of 128: 53 us, 5.2 TB/s;
-// 4096 x 4096: 6.4 us, of which the tokens' digits, the first weights and the end of the only unit are latency; eight
-// tokens, 4096 x 14336: 26 us.  With eight tokens the issue rate bounds it (about 215 instructions a KB of codes, 1.8 a cycle).
+// Measured in a chain of calls, weights from HBM (6.57 TB/s copied): one token, 131072 x 4096 with groups of 128: 52 us, 5.3 TB/s;
+// 4096 x 4096: 6.3 us, of which the tokens' digits, the first weights and the end of the only unit are latency; eight
+// tokens, 4096 x 14336: 23 us.  With eight tokens the issue rate bounds it (about 215 instructions a KB of codes, 1.8 a cycle).
 // ----------------------------------------------------------------------------
 constexpr int kRowThreads = 512;
 constexpr int kRowWarps = kRowThreads / 32;
@@ -789,7 +789,7 @@ union_kernel(const int* __restrict__ sel, int stride, const int* __restrict__ co
 // through L1), the other warps and the S blocks of a cluster split the entries; their sums meet in the cluster's shared memory,
 // in a fixed order: results do not depend on timing.
 //
-// Measured: 3 us of the 15 us of Stage 2 of 4096 x 12288 with 2867 channels and one token once the h are there; 50 us for 8192 x
+// Measured: 3 us of the 14 us of Stage 2 of 4096 x 12288 with 2867 channels and one token once the h are there; 50 us for 8192 x
 // 28672 and eight tokens (106 MB, 2.1 TB/s): four columns of digits a token make it bound by the issue rate.
 // ----------------------------------------------------------------------------
 __host__ __device__ constexpr int down_threads(int nt) { return nt >= 3 ? 256 : 512; }   // 32 sums a thread and 8 columns of digits
