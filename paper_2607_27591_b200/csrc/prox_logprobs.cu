@@ -38,7 +38,6 @@ extern "C" prox_status_t prox_token_logprobs(const void* logits_dev, int dtype, 
   a.x = static_cast<const uint8_t*>(logits_dev);
   a.row_bytes = (long long)row_stride * size;
   a.V = V;
-  a.temperature = temperature;
   a.inv_temperature = 1.0f / temperature;
   a.given = given_dev; a.n_given = n_given; a.logprob = logprob_dev; a.entropy = entropy_dev_or_null;
   a.k = n_top; a.top_logprob = top_logprob_dev; a.top_index = top_index_dev;

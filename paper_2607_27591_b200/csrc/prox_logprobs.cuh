@@ -39,7 +39,7 @@ struct Args {
   const uint8_t* x;
   long long row_bytes;     // from one row to the next
   int V;
-  float temperature, inv_temperature;
+  float inv_temperature;
   const int* given;        // [T][n_given]
   int n_given;
   float* logprob;          // [T][n_given]

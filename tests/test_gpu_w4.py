@@ -81,6 +81,7 @@ LINEAR = [  # N, K, group, B, zeros, x type, y type
     (1024, 1024, 0, 3, True, 0, 1), (5003, 1376, 32, 3, True, 2, 2), (4096, 4096, 128, 8, False, 0, 1), (4097, 4096, 64, 5, True, 0, 0),
     (130, 14336, 128, 8, False, 0, 1), (4096, 14336, 128, 16, True, 0, 1), (64, 65536, 128, 16, False, 0, 1), (333, 4128, 128, 17, True, 0, 1),
     (300, 4096, 32, 33, False, 2, 1), (20011, 2048, 64, 1, True, 2, 1), (257, 8160, 0, 13, False, 0, 1), (2500, 512, 128, 1, True, 0, 1),
+    (40, 320, 64, 4, True, 2, 1), (70, 1696, 32, 6, True, 0, 1), (3000, 192, 64, 2, False, 0, 1), (19, 12800, 0, 8, True, 0, 1), (2368, 16384, 64, 8, True, 0, 1),
 ]
 
 
@@ -252,6 +253,7 @@ FFN = [  # D, F, k2, group, B, zeros, y type
     (384, 1000, 17, 128, 2, False, 1), (1024, 2752, 700, 128, 1, True, 1), (4096, 12288, 2867, 128, 1, False, 1), (4096, 12288, 2867, 128, 4, False, 0),
     (8192, 2048, 512, 128, 8, True, 1), (16384, 704, 350, 128, 8, False, 1), (16384, 704, 9, 0, 1, True, 1), (640, 65536, 6000, 128, 2, False, 1),
     (2048, 5504, 5504, 0, 5, False, 1), (1152, 3008, 1203, 128, 6, False, 1), (256, 333, 100, 128, 7, True, 1),
+    (384, 1000, 200, 128, 3, True, 1), (1152, 640, 333, 128, 8, True, 0), (640, 2000, 1999, 0, 2, True, 1), (16384, 1024, 900, 128, 7, True, 1), (128, 65536, 65536, 128, 1, True, 1),
 ]
 
 
