@@ -101,8 +101,8 @@ __device__ __forceinline__ float exp2_fast(float v) {
   return r;
 }
 // 2^-256 is 0: what lies that far below, or is -inf, counts as nothing (and is kept from making 0 * infinity in w).
-// fmaxf drops what is no number; the maximum keeps it (max_nan), and a maximum that is no number or infinite makes results
-// that are no numbers.
+// fmaxf drops what is no number; the maximum keeps it, in a round and from round to round (max_nan), and a maximum that is no
+// number or infinite makes results that are no numbers.
 __device__ __forceinline__ float clamp_low(float d) { return fmaxf(d, -256.f); }
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const Args a) {
     float most = vector_max[0];
 #pragma unroll
     for (int j = 1; j < kVectors; ++j) most = max_nan(most, vector_max[j]);
-    if (!(most <= sum.m)) raise(sum, most, c);
+    if (!(most <= sum.m)) raise(sum, max_nan(sum.m, most), c);   // (a maximum that is no number stays one)
     {
       uint64_t s2 = pair(0.f, 0.f), w2 = s2;
       const uint64_t minus_m = pair(-sum.m, -sum.m), c2 = pair(c, c);
