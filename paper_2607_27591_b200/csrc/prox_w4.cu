@@ -8,12 +8,10 @@ using namespace prox;
 
 namespace {
 
-constexpr int kMaxSmem = kMaxBlockSmem - 8192;   // dynamic; the kernels have up to 8 KB of their own
+using w4::kMaxSmem;
+static_assert(kMaxSmem == kMaxBlockSmem - 8192, "what host_allow_smem asks for");
 constexpr int kMaxRowBlocks = 256;       // of the gate and up kernel
 constexpr int kFfnTokens = 8;            // tokens of a call of the sparse FFN, as everywhere in the library
-
-// Shape of a launch of rows_kernel for `tiles` tiles of 16 rows.
-struct RowsPlan { int S, WM, WK, stages, R, grid; size_t smem; };
 
 // Clusters of S blocks that the GPU holds at once (a block of these kernels has an SM to itself).
 template <auto Kern>
@@ -34,40 +32,14 @@ int clusters_at_once(int device, int S, int threads, size_t smem) {
   return n;
 }
 
-// The shape that is done first, in cycles: an SM takes about 48 for 128 columns of a tile when all its warps are busy (18
-// more for every 8 further columns of digits), a warp alone 400 (150 more); the end of a unit costs 1500, much less where no warp waits for
-// another, the cluster's sum 5000; a token's digits are made at 4 inputs a cycle.
-RowsPlan plan_rows(int tiles, int K, int B, int words, int nt, int sms, int dev) {
-  const int C = (K + 127) / 128;
-  RowsPlan best = {};
-  double least = 1e30;
-  for (int S = 1; S <= 8; S *= 2) {
-    const int Cs = w4::rows_share(C, S);
-    const int at_once = S == 1 ? sms : std::min(sms / S, clusters_at_once<w4::rows_kernel<4, 1, false, false>>(dev, S, w4::kRowThreads, 120 * 1024));
-    if (S > 1 && Cs * (S - 1) >= C) break;                   // a block without columns
-    for (int WK = 1; WK <= w4::kRowWarps && WK <= 2 * Cs - 1; WK *= 2)
-      for (int WM = w4::kRowWarps / WK; WM >= 1; WM /= 2)
-        for (int stages : {w4::kMaxStages, 3, 2}) {
-          const size_t sum = S > 1 ? (size_t)WM * 64 * B : 0;  // a unit's sums, kept for the cluster
-          const size_t fixed = w4::rows_fixed_bytes(Cs, nt, words) + (WK > 1 ? w4::rows_red_bytes(nt) : 0) +
-                               (size_t)w4::kRowWarps * stages * w4::rows_stage_bytes(words);
-          if (fixed + sum > (size_t)kMaxSmem) continue;
-          const int clusters = std::max(1, std::min(tiles, at_once)), most = (tiles + clusters - 1) / clusters, mine = (most + WM - 1) / WM;
-          const int R = S > 1 ? (int)std::min<size_t>(std::min(mine, 16), (kMaxSmem - fixed) / sum) : 0;
-          const double cost = std::max((double)most * Cs * (30 + 18 * nt), (double)mine * w4::rows_run(Cs, WK) * (250 + 150 * nt)) * (1.0 + 0.3 / stages) +
-                              mine * (WK == 1 ? 300.0 : 1500.0) + (S > 1 ? 5000.0 * ((mine + R - 1) / R) : 0.0) + Cs * 32.0 * B;
-          if (cost < least - 1e-9) {
-            least = cost;
-            best = {S, WM, WK, stages, R, clusters * S, fixed + R * sum};
-          }
-          break;                                               // (the most stages that fit)
-        }
-  }
-  return best;
+w4::RowsPlan plan_rows(int tiles, int K, int B, int words, int sms, int dev) {
+  return w4::plan_rows(tiles, K, B, words, (B + 1) / 2, sms, [dev](int S) {
+    return clusters_at_once<w4::rows_kernel<4, 1, false, false>>(dev, S, w4::kRowThreads, 120 * 1024);
+  });
 }
 
 template <int W, bool ZP, bool GATEUP>
-cudaError_t launch_rows(const w4::RowsArgs& a, int nt, const RowsPlan& p, int dev, cudaStream_t st) {
+cudaError_t launch_rows(const w4::RowsArgs& a, int nt, const w4::RowsPlan& p, int dev, cudaStream_t st) {
   switch (nt) {
     case 1: return host_launch<w4::rows_kernel<W, 1, ZP, GATEUP>>(dev, p.grid, w4::kRowThreads, p.smem, p.S, st, a);
     case 2: return host_launch<w4::rows_kernel<W, 2, ZP, GATEUP>>(dev, p.grid, w4::kRowThreads, p.smem, p.S, st, a);
@@ -77,7 +49,7 @@ cudaError_t launch_rows(const w4::RowsArgs& a, int nt, const RowsPlan& p, int de
 }
 
 template <int W>
-cudaError_t launch_linear(const w4::RowsArgs& a, int nt, const RowsPlan& p, int dev, cudaStream_t st) {
+cudaError_t launch_linear(const w4::RowsArgs& a, int nt, const w4::RowsPlan& p, int dev, cudaStream_t st) {
   return a.w.zeros ? launch_rows<W, true, false>(a, nt, p, dev, st) : launch_rows<W, false, false>(a, nt, p, dev, st);
 }
 
@@ -178,16 +150,15 @@ prox_status_t prox_w4_linear(const prox_w4_t* w, int N, int K, int group_size, c
   a.x_vec = host_aligned(x_dev, 16) && (B == 1 || x_stride % 8 == 0);
   const size_t ysize = y_dtype == w4::kFp32 ? 4 : 2;
   const int words = group_size == 32 ? 1 : group_size == 64 ? 2 : 4;
-  // as many tokens a pass as fit in the shared memory of a cluster
-  const int Cs = w4::rows_share((K + 127) / 128, 8);
-  int per = w4::kMaxPass;
-  while (per > 1 && w4::rows_fixed_bytes(Cs, (per + 1) / 2, words) + 32 * w4::rows_stage_bytes(words) + 16 * 64 * per > (size_t)kMaxSmem) --per;
+  auto plan = [&](int tokens) { return plan_rows((N + 15) / 16, K, tokens, words, sms, dev); };
+  const int per = w4::linear_pass(B, K, words, plan);
+  if (per < 1) return PROX_ERR_UNSUPPORTED;                // before anything is written
   for (int b = 0; b < B; b += per) {
     a.B = std::min(per, B - b);
     a.x = static_cast<const uint16_t*>(x_dev) + (size_t)b * x_stride;
     a.y = static_cast<uint8_t*>(y_dev) + (size_t)b * y_stride * ysize;
     const int nt = (a.B + 1) / 2;
-    const RowsPlan p = plan_rows((N + 15) / 16, K, a.B, words, nt, sms, dev);
+    const w4::RowsPlan p = plan(a.B);
     a.S = p.S; a.WM = p.WM; a.WK = p.WK; a.stages = p.stages; a.R = p.R;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     CKL(words == 4 ? launch_linear<4>(a, nt, p, dev, st) : words == 2 ? launch_linear<2>(a, nt, p, dev, st) : launch_linear<1>(a, nt, p, dev, st));
@@ -230,14 +201,15 @@ prox_status_t prox_w4_stage2_ffn(const prox_w4_t* gate, const prox_w4_t* up, con
   const int* list = sel_dev;
   const int* count = count_dev_or_null;
   const uint8_t* members = nullptr;
-  int most = k2;                            // channels that some token keeps, at most
+  const int most = B > 1 ? (int)std::min<long long>(F, (long long)B * k2) : k2;   // channels that some token keeps, at most
+  const w4::RowsPlan p = plan_rows(std::max(1, (most + 7) / 8), D, B, 4, std::min(sms, kMaxRowBlocks), dev);
+  if (!p.grid) return PROX_ERR_UNSUPPORTED;                // before anything is written
   if (B > 1) {
     int* ulist = reinterpret_cast<int*>(wsp + ws.list);
     int* ucount = reinterpret_cast<int*>(wsp + ws.count);
     CKL(host_launch<w4::union_kernel>(dev, w4::kUnionBlocks, w4::kUnionThreads, ((size_t)F + 31) / 32 * 4, w4::kUnionBlocks, st, sel_dev, sel_stride, count_dev_or_null, k2, B, F, ulist,
                wsp + ws.members, ucount));
     list = ulist; count = ucount; members = wsp + ws.members;
-    most = (int)std::min<long long>(F, (long long)B * k2);
   }
   const int groups = groups_of(D, group_size);
   w4::RowsArgs a = {};
@@ -247,7 +219,6 @@ prox_status_t prox_w4_stage2_ffn(const prox_w4_t* gate, const prox_w4_t* up, con
   a.list = list; a.count = count; a.n = most; a.members = members; a.h = h;
   a.hmax = reinterpret_cast<unsigned*>(wsp + ws.hmax);
   const int nt = (B + 1) / 2;
-  const RowsPlan p = plan_rows(std::max(1, (most + 7) / 8), D, B, 4, nt, std::min(sms, kMaxRowBlocks), dev);
   a.S = p.S; a.WM = p.WM; a.WK = p.WK; a.stages = p.stages; a.R = p.R;
   CKL(gate->zeros ? launch_rows<4, true, true>(a, nt, p, dev, st) : launch_rows<4, false, true>(a, nt, p, dev, st));
   w4::DownArgs d = {};

@@ -28,6 +28,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "prox_w4_plan.h"
+
 namespace prox {
 namespace w4 {
 
@@ -141,12 +143,6 @@ __device__ __forceinline__ void cluster_barrier() {
 // 4096 x 4096: 6.3 us, of which the tokens' digits, the first weights and the end of the only unit are latency; eight
 // tokens, 4096 x 14336: 23 us.  With eight tokens the issue rate bounds it (about 215 instructions a KB of codes, 1.8 a cycle).
 // ----------------------------------------------------------------------------
-constexpr int kRowThreads = 512;
-constexpr int kRowWarps = kRowThreads / 32;
-constexpr int kBatch = 2;                // chunks that a warp asks for at a time: a 128-byte line of each of 16 rows
-constexpr int kMaxStages = 5;            // batches of a warp in shared memory, at most (sid has room for them)
-constexpr int kMaxPass = 8;              // tokens of a pass over the weights: 32 columns of digits
-
 struct RowsArgs {
   Mat w, w2;               // linear: w.  gate and up: w and w2
   int rows, K, groups, gstep;   // gstep 0: one scale per row
@@ -166,29 +162,6 @@ struct RowsArgs {
   int x_half;              // x is fp16 (else bf16)
   int x_vec;               // x rows start on 16-byte boundaries
 };
-
-// A warp's stage: a batch of its 16 rows (codes with a gap behind every row, so that lanes of one load do not meet), their scales
-// and zero points (with room for where an element lies in its word).
-template <int W>
-struct Stage {
-  static constexpr int kGroups = kBatch * 4 / W;
-  static constexpr int kPitch = kBatch * 64 + 16 * W;
-  static constexpr int kScales = W == 4 ? 8 : W == 2 ? 16 : 32;         // bytes of a row
-  static constexpr int kZeros = W == 1 ? 16 : 8;
-  static constexpr int kAtScales = 16 * kPitch, kAtZeros = kAtScales + 16 * kScales, kBytes = kAtZeros + 16 * kZeros;
-};
-__host__ __device__ constexpr int rows_stage_bytes(int words) { return words == 4 ? Stage<4>::kBytes : words == 2 ? Stage<2>::kBytes : Stage<1>::kBytes; }
-
-// Chunks of a block of a cluster, of a warp along the columns: whole batches
-__host__ __device__ constexpr int rows_share(int C, int S) { return S == 1 ? C : ((C + S - 1) / S + kBatch - 1) / kBatch * kBatch; }
-__host__ __device__ constexpr int rows_run(int Cs, int WK) { return ((Cs + WK - 1) / WK + kBatch - 1) / kBatch * kBatch; }
-
-// Shared memory behind the tokens' digits: what comes off a group's sums, the warps' stages, their partial tiles, the block's sums
-__host__ __device__ constexpr size_t rows_digit_bytes(int chunks, int nt) { return (size_t)chunks * 1024 * nt; }
-__host__ __device__ constexpr size_t rows_fixed_bytes(int chunks, int nt, int words) {
-  return rows_digit_bytes(chunks, nt) + (size_t)chunks * (4 / words) * 64 * nt;
-}
-__host__ __device__ constexpr size_t rows_red_bytes(int nt) { return (size_t)2 * kRowWarps * nt * 512; }   // only where WK > 1
 
 __device__ __forceinline__ void inputs_of(float (&f)[8], const uint4& v, bool half) {
   const uint32_t e[4] = {v.x, v.y, v.z, v.w};
