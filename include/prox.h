@@ -205,6 +205,13 @@ prox_status_t prox_ffn_last_mask(prox_ffn_t* h, int B, int k2, int32_t* sel_dev,
 prox_status_t prox_ffn_forward_host(prox_ffn_t* h, const void* x_host, int B, int k1, int k2,
                                     void* y_host, void* stream);
 
+/* Loads the code of the calls that need no handle (prox_stage2_ffn_noalloc, prox_w4_*, prox_token_logprobs) on the
+ * current device.  These calls allocate nothing themselves, but CUDA loads a kernel's code when the kernel is first
+ * used, and may take device memory for it (2 MB at a time).  After this call, or after prox_ffn_create, which makes
+ * it, it has all it needs.  Once per device and process; later calls return at once.  Not under stream capture.
+ * Errors: OOM, CUDA. */
+prox_status_t prox_load_kernels(void);
+
 /* Stage 2 for callers that must not allocate device memory.
  * (The paper has no counterpart; this is a packaging variant of prox_stage2_ffn.)
  *
@@ -228,10 +235,12 @@ prox_status_t prox_ffn_forward_host(prox_ffn_t* h, const void* x_host, int B, in
  * y) live in a 192 KB array that is part of the library image on every GPU that
  * loads it, instead of in allocated memory.  Hence the limits: d_model <= 16384
  * and k2 <= 32768 (PROX_ERR_UNSUPPORTED beyond; use the handle-based call).
- * No cudaMalloc, cudaFree or allocating library routine is called.
+ * No cudaMalloc, cudaFree or allocating library routine is called; CUDA's own
+ * loading of the kernels on their first use is over once prox_load_kernels (or
+ * prox_ffn_create) has been called.
  *
- * The first call on a device looks up the device address of that array (the
- * device must be current); make that first call outside any stream capture.
+ * The first call on a device (or prox_load_kernels) looks up the device address
+ * of that array (the device must be current); make it outside any stream capture.
  * All calls on a device share the one array and it keeps the last call's
  * contents (the accumulator is cleared at the start of every call): two calls
  * that overlap on the GPU - different streams, or concurrent host threads -
@@ -346,7 +355,8 @@ prox_status_t prox_rmsnorm(prox_ffn_t* h, const float* x_res_dev, const void* no
 
 /* ---- Weights held in 4 bits.  The proxies above only rank channels; these calls compute with 4-bit weights (the
  * low-bit Stage-2 weights under sparsity that the paper leaves to future work, and the projections around
- * the FFN of a checkpoint in that form).  None needs a handle, and none allocates.  A matrix [rows, cols] is
+ * the FFN of a checkpoint in that form).  None needs a handle, and none allocates
+ * (prox_load_kernels: what CUDA takes on their first use).  A matrix [rows, cols] is
  *     w[r, c] = scale[r, c / G] * (code[r, c] - zero[r, c / G]),   G = group_size, or cols where that is 0
  *   codes   dev uint8 [rows, cols / 2], 16-byte aligned: byte i holds column 2i in bits 0-3, column 2i + 1 in bits 4-7
  *   scales  dev fp16 [rows, groups], groups = ceil(cols / G) (the last group may be shorter), 16-byte aligned

@@ -87,6 +87,7 @@ _SIGS = {
     "prox_calib_histogram": [_vp, C.POINTER(C.c_int64), C.POINTER(_f)],
     "prox_calib_seen": [_vp, C.POINTER(C.c_int64), C.POINTER(C.c_int64)],
     "prox_rmsnorm": [_vp, _vp, _vp, _d, _i, _vp, _vp],
+    "prox_load_kernels": [],
     "prox_w4_quantize": [_vp, _i, _i, _i, _vp, _vp, _vp],
     "prox_w4_linear": [C.POINTER(ProxW4), _i, _i, _i, _vp, C.c_int64, _i, _i, _vp, C.c_int64, _i, _vp],
     "prox_w4_stage2_workspace": [_i, _i, _i, C.POINTER(C.c_int64)],
@@ -298,6 +299,10 @@ def prox_calib_seen(calib: int):
 
 def prox_rmsnorm(handle: int, x_res, norm_w, eps: float, B: int, xn_out, stream=None) -> None:
     _check(_lib.prox_rmsnorm(handle, _ptr(x_res), _ptr(norm_w), eps, B, _ptr(xn_out), _ptr(stream)), "prox_rmsnorm")
+
+
+def prox_load_kernels() -> None:
+    _check(_lib.prox_load_kernels(), "prox_load_kernels")
 
 
 def _w4(w) -> ProxW4:

@@ -3,6 +3,7 @@
 #include "prox_host.h"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdio>
 #include <cstdlib>
@@ -855,6 +856,20 @@ prox_status_t reset_shared_state(prox_ffn* h, cudaStream_t st) {
 // ============================================================================
 extern "C" {
 
+prox_status_t prox_load_kernels(void) {
+  static std::atomic<uint64_t> loaded{0};                    // a bit per device
+  int dev;
+  cudaError_t e = cudaGetDevice(&dev);
+  const uint64_t bit = e == cudaSuccess && dev < 64 ? 1ull << dev : 0;
+  if (e == cudaSuccess && (loaded.load(std::memory_order_acquire) & bit)) return PROX_OK;
+  if (e == cudaSuccess) e = prox_noalloc_load(dev);
+  if (e == cudaSuccess) e = prox::host_load_w4();
+  if (e == cudaSuccess) e = prox::host_load_logprobs();
+  if (e != cudaSuccess) return map_cuda(e);
+  loaded.fetch_or(bit, std::memory_order_release);
+  return PROX_OK;
+}
+
 prox_status_t prox_ffn_create(const prox_ffn_config_t* cfg, const void* w_gate, const void* w_up,
                               const void* w_down, void* stream, prox_ffn_t** out) {
   (void)stream;
@@ -879,7 +894,8 @@ prox_status_t prox_ffn_create(const prox_ffn_config_t* cfg, const void* w_gate, 
   h->wd = static_cast<const uint16_t*>(w_down);
   cudaError_t e = cudaGetDevice(&h->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->sm_count, cudaDevAttrMultiProcessorCount, h->device);
-  if (e != cudaSuccess) { delete h; return PROX_ERR_CUDA; }
+  if (e != cudaSuccess) { delete h->prof; delete h; return PROX_ERR_CUDA; }
+  if (const prox_status_t s = prox_load_kernels()) { delete h->prof; delete h; return s; }
 
   const int D = cfg->d_model, F = cfg->d_ff, MB = cfg->max_batch;
   const int ns_max = nstrips_for(F, 8);            // of the integer formats (16 bits: twice as many, of a quarter of the sums each)

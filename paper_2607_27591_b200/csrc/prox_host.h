@@ -6,6 +6,8 @@
 
 #include "prox.h"
 
+cudaError_t prox_noalloc_load(int device);
+
 namespace prox {
 
 // Records a CUDA error for prox_last_cuda_error and gives the status for it (prox_api.cu).
@@ -35,6 +37,19 @@ inline int host_sm_count(int device) {
   }
   return n;
 }
+
+// Loads the code of kernels on the current device.  (CUDA does so at a kernel's first launch otherwise, and may take device memory
+// for it.)
+template <auto... Kerns>
+cudaError_t host_load() {
+  cudaError_t e = cudaSuccess;
+  cudaFuncAttributes at;
+  ((e = e == cudaSuccess ? cudaFuncGetAttributes(&at, reinterpret_cast<const void*>(Kerns)) : e), ...);
+  return e;
+}
+// ... those of the calls without a handle (prox_w4.cu, prox_logprobs.cu; prox_noalloc.cu: prox_noalloc_load above)
+cudaError_t host_load_w4();
+cudaError_t host_load_logprobs();
 
 constexpr int kMaxBlockSmem = 227 * 1024;
 

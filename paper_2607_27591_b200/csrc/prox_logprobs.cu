@@ -14,6 +14,11 @@ cudaError_t launch_logprobs(const lp::Args& a, unsigned grid, int dev, cudaStrea
 
 }  // namespace
 
+cudaError_t prox::host_load_logprobs() {
+  return host_load<lp::logprobs_kernel<lp::kBf16, false>, lp::logprobs_kernel<lp::kBf16, true>, lp::logprobs_kernel<lp::kFp16, false>,
+                   lp::logprobs_kernel<lp::kFp16, true>, lp::logprobs_kernel<lp::kFp32, false>, lp::logprobs_kernel<lp::kFp32, true>>();
+}
+
 extern "C" prox_status_t prox_token_logprobs(const void* logits_dev, int dtype, int T, int V, int64_t row_stride, float temperature,
                                              const int32_t* given_dev, int n_given, float* logprob_dev, float* entropy_dev_or_null,
                                              int n_top, float* top_logprob_dev, int32_t* top_index_dev, void* stream) {

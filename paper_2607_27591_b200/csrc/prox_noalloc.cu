@@ -35,7 +35,37 @@ int g_sm_count[kMaxDevices];
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Once per device, which is current: the device address of the static array.  Not something to do under stream capture.
+cudaError_t set_up(int dev) {
+  std::lock_guard<std::mutex> lock(g_setup_mutex);
+  if (g_scratch_dev[dev]) return cudaSuccess;
+  void* p = nullptr;
+  int n = 0;
+  cudaError_t e = cudaGetSymbolAddress(&p, g_noalloc_scratch);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess || !p || n < 1) {
+    (void)cudaGetLastError();
+    return e != cudaSuccess ? e : cudaErrorUnknown;
+  }
+  g_sm_count[dev] = n;
+  g_scratch_dev[dev] = static_cast<float*>(p);
+  return cudaSuccess;
+}
+
 }  // namespace
+
+// Declared in prox_host.h (which would bring a second namespace `prox` in here).
+cudaError_t prox_noalloc_load(int dev) {
+  if (dev >= kMaxDevices) return cudaSuccess;                // (prox_stage2_ffn_noalloc refuses such a device)
+  if (const cudaError_t e = set_up(dev)) return e;
+  const void* kernels[] = {reinterpret_cast<const void*>(prox::gateup_kernel), reinterpret_cast<const void*>(prox::down_kernel),
+                           reinterpret_cast<const void*>(prox::finalize_kernel)};
+  for (const void* k : kernels) {
+    cudaFuncAttributes at;
+    if (const cudaError_t e = cudaFuncGetAttributes(&at, k)) return e;
+  }
+  return cudaSuccess;
+}
 
 extern "C" prox_status_t prox_stage2_ffn_noalloc(const void* x_dev, const void* w_gate_dev,
                                                  const void* w_up_dev, const void* w_down_t_dev,
@@ -54,30 +84,9 @@ extern "C" prox_status_t prox_stage2_ffn_noalloc(const void* x_dev, const void* 
 
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return PROX_ERR_CUDA;
-  float* scratch = nullptr;
-  int sms = 0;
-  {
-    std::lock_guard<std::mutex> lock(g_setup_mutex);
-    if (!g_scratch_dev[dev]) {
-      // First call on this device (which is current): resolve the device address of
-      // the static array once.  This is set-up work, not something to do under
-      // stream capture.
-      void* p = nullptr;
-      if (cudaGetSymbolAddress(&p, g_noalloc_scratch) != cudaSuccess || !p) {
-        (void)cudaGetLastError();
-        return PROX_ERR_CUDA;
-      }
-      int n = 0;
-      if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
-        (void)cudaGetLastError();
-        return PROX_ERR_CUDA;
-      }
-      g_sm_count[dev] = n;
-      g_scratch_dev[dev] = static_cast<float*>(p);
-    }
-    scratch = g_scratch_dev[dev];
-    sms = g_sm_count[dev];
-  }
+  if (set_up(dev) != cudaSuccess) return PROX_ERR_CUDA;
+  float* scratch = g_scratch_dev[dev];
+  const int sms = g_sm_count[dev];
   float* hbuf = scratch;                          // [k2]
   float* yacc = scratch + kNoAllocMaxK2;          // [d_model]
   cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -104,7 +104,26 @@ cudaError_t launch_down(w4::DownArgs& a, int dev, cudaStream_t st) {
   return a.w.zeros ? launch_down<NT, true>(a, dev, st) : launch_down<NT, false>(a, dev, st);
 }
 
+template <int W, bool ZP, bool GATEUP>
+cudaError_t load_rows() {
+  return host_load<w4::rows_kernel<W, 1, ZP, GATEUP>, w4::rows_kernel<W, 2, ZP, GATEUP>, w4::rows_kernel<W, 3, ZP, GATEUP>,
+                   w4::rows_kernel<W, 4, ZP, GATEUP>>();
+}
+
+template <bool ZP>
+cudaError_t load_zero_points() {   // kernels of matrices with zero points, or without
+  for (cudaError_t (*load)() : {load_rows<1, ZP, false>, load_rows<2, ZP, false>, load_rows<4, ZP, false>, load_rows<4, ZP, true>})
+    if (const cudaError_t e = load()) return e;
+  return host_load<w4::down_kernel<1, ZP>, w4::down_kernel<2, ZP>, w4::down_kernel<3, ZP>, w4::down_kernel<4, ZP>>();
+}
+
 }  // namespace
+
+cudaError_t prox::host_load_w4() {
+  if (const cudaError_t e = load_zero_points<false>()) return e;
+  if (const cudaError_t e = load_zero_points<true>()) return e;
+  return host_load<w4::union_kernel, w4::quantize_kernel>();
+}
 
 #define CKL(...)                                        \
   do {                                                   \

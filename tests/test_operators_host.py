@@ -98,3 +98,12 @@ def test_binding_raises(pb):
         pb.prox_token_logprobs(None, 0, 1, 1, 1, 1.0, None, 0, None, None, 0, None, None)
     with pytest.raises(pb.ProxError):
         pb.prox_w4_linear((P, P, None), 0, 64, 32, P, 64, 0, 1, P, 1, 0)
+
+
+def test_loading_kernels_without_a_gpu_says_so(pb):
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("there is a GPU")
+    assert pb.raw("prox_load_kernels")() == 4
+    with pytest.raises(pb.ProxError):
+        pb.prox_load_kernels()
