@@ -728,7 +728,8 @@ union_kernel(const int* __restrict__ sel, int stride, const int* __restrict__ co
 // M = columns, K = list entries, N = digits of the tokens' h s.  A warp owns 128 columns (one scale group) and takes
 // tiles of 32 entries: 64 bytes of each of 32 rows, copied to its own stages in shared memory with what else the tile needs
 // (scales, zero points, h); four rows' bytes are transposed into A registers.  h s is a fixed-point number, and one
-// whole-number sum runs over all tiles: |digit| <= 128, 16 q <= 240, at most 32768 entries, below 2^30.  Its exponent is the
+// whole-number sum runs over all tiles: |digit| <= 128, 16 q <= 240, at most 32768 entries, below 2^30.  (h is taken below 1 by a power
+// of two first, so that no exponent is out of reach.)  Its exponent is the
 // warp's and the token's: 30 bits are room for the token's largest |h|, which the kernel before this has left, times four times
 // the largest scale of the warp's first tile.  Where a tile brings a scale above that, the exponents fall and the numbers
 // that the sums so far stand for are shifted down.
@@ -755,6 +756,10 @@ struct DownArgs {
   int y_type;
   int WC, S;
 };
+
+// Exponent that takes numbers up to the fp32 magnitude whose bits are `most` below 1 (below 4 at fp32's upper end): their
+// products with scales neither overflow nor run out of exponents.
+__device__ __forceinline__ int unit_exponent(uint32_t most) { return max(126 - max((int)(most >> 23), 1), -126); }
 
 // bytes of a stage: 32 rows of codes, a word each of scales, zero points and where to look in them, h
 __host__ __device__ constexpr int down_stage(int B) { return 2048 + 128 + 128 + 128 + 128 * B; }
@@ -845,12 +850,17 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
     if (m > hm[i % B]) atomicMax(hm + i % B, m);
   }
   __syncthreads();
-  int token[NT], power[NT][2];                                 // fixed point of tokens 2 i and 2 i + 1: h s times 2^power
+  int token[NT], power[NT][2];                                 // fixed point of tokens 2 i and 2 i + 1: 2^hexp h s times 2^power
+  float hscale[NT];                                            // 2^hexp of the lane's tokens
   uint32_t most_scale = 0;                                     // bits of the scale that there is room for; 0: no sums yet
 #pragma unroll
-  for (int i = 0; i < NT; ++i) token[i] = min(i * 2 + (g >> 2), B - 1);   // columns behind the last token: computed, never used
-  auto power_of = [&](int b) {                                 // (of a product that is rounded: one bit of room)
-    return min(fixed_exponent(__float_as_uint(__uint_as_float(hm[min(b, B - 1)]) * __uint_as_float(most_scale)) & 0x7fffffffu) + 3, 126);
+  for (int i = 0; i < NT; ++i) {
+    token[i] = min(i * 2 + (g >> 2), B - 1);                   // columns behind the last token: computed, never used
+    hscale[i] = pow2(unit_exponent(hm[token[i]]));
+  }
+  auto power_of = [&](int b) {                                 // (of a product that is rounded: one bit of room; 126: of h that are all 0)
+    const unsigned most = hm[min(b, B - 1)];
+    return min(fixed_exponent(__float_as_uint(__uint_as_float(most) * pow2(unit_exponent(most)) * __uint_as_float(most_scale)) & 0x7fffffffu) + 3, 126);
   };
 
   int acc[8][NT][4], zacc[NT][4];                              // even columns (rows g): sums of q, odd ones (g + 8): of 16 q
@@ -892,7 +902,7 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       const float2 h = *reinterpret_cast<const float2*>(st + 2432 + token[i] * 128 + t * 32 + r0 * 4);
-      const float v0 = in0 ? h.x * s0 : 0.f, v1 = in1 ? h.y * s1 : 0.f;
+      const float v0 = in0 ? h.x * hscale[i] * s0 : 0.f, v1 = in1 ? h.y * hscale[i] * s1 : 0.f;
       const float factor = pow2(g < 4 ? power[i][0] : power[i][1]);
       const uint32_t d0 = digits(__float2int_rn(v0 * factor)), d1 = digits(__float2int_rn(v1 * factor));
       // bytes 0, 1 of both numbers, and bytes 2, 3: lanes of digits 0, 1 keep the former and get those of the lane two further on
@@ -967,8 +977,9 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     const int b = i * 2 + (t >> 1);                            // lane t has digits 0, 1 (t even) or 2, 3 (t odd) of the token
-    const int e = most_scale ? -(t & 2 ? power[i][1] : power[i][0]) : 0, e0 = max(-126, min(126, e));
-    const float f0 = hm[min(b, B - 1)] >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : pow2(e0), f1 = pow2(max(-126, min(126, e - e0)));
+    const unsigned most = hm[min(b, B - 1)];
+    const int e = most_scale ? -(t & 2 ? power[i][1] : power[i][0]) - unit_exponent(most) : 0, e0 = max(-126, min(126, e));
+    const float f0 = most >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : pow2(e0), f1 = pow2(max(-126, min(126, e - e0)));
     float* at = red + (size_t)wr * outs + b * width + wc * 128 + g * 16 + (t & 1);
 #pragma unroll
     for (int m = 0; m < 8; ++m) {                              // columns g * 16 + 2 m (even lanes), + 1 (odd lanes) of the warp's
