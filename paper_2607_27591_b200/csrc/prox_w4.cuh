@@ -729,10 +729,12 @@ union_kernel(const int* __restrict__ sel, int stride, const int* __restrict__ co
 // tiles of 32 entries: 64 bytes of each of 32 rows, copied to its own stages in shared memory with what else the tile needs
 // (scales, zero points, h); four rows' bytes are transposed into A registers.  h s is a fixed-point number, and one
 // whole-number sum runs over all tiles: |digit| <= 128, 16 q <= 240, at most 32768 entries, below 2^30.  (h is taken below 1 by a power
-// of two first, so that no exponent is out of reach.)  Its exponent is the
-// warp's and the token's: 30 bits are room for the token's largest |h|, which the kernel before this has left, times four times
-// the largest scale of the warp's first tile.  Where a tile brings a scale above that, the exponents fall and the numbers
-// that the sums so far stand for are shifted down.
+// of two first, so that no exponent is out of reach.)  Its exponent is the warp's and the token's: 30 bits are room for 4 times
+// the token's largest |h s| in the warp's first tile, times what the list's largest |h| (which the kernel before this has left) is
+// above the tile's, 64 times in all at most.  Where a tile brings a product that there is no room for, the token's exponent falls to make
+// such room above it, and the numbers that its sums so far stand for are shifted down.  So a product is off by 2^-24 of the token's
+// largest in its warp at most, and by 2^-27 of its largest |h| times its largest scale.  Channels that other tokens keep, or that are
+// skipped, do not count.
 // WC warps of a block are side by side in the columns (what they read of h and of the scales' sectors they share
 // through L1), the other warps and the S blocks of a cluster split the entries; their sums meet in the cluster's shared memory,
 // in a fixed order: results do not depend on timing.
@@ -742,6 +744,9 @@ union_kernel(const int* __restrict__ sel, int stride, const int* __restrict__ co
 // ----------------------------------------------------------------------------
 __host__ __device__ constexpr int down_threads(int nt) { return nt >= 3 ? 256 : 512; }   // 32 sums a thread and 8 columns of digits
 __host__ __device__ constexpr int down_stages(int nt) { return nt >= 3 ? 6 : 4; }        // 12 KB of codes a warp in flight, or 8
+
+constexpr int kMaxPower = 120;           // of fixed-point numbers: what lies below 2^-90 of the largest |h| loses bits
+constexpr int kMaxRoom = 6;              // bits kept free above the largest product so far, at most
 
 struct DownArgs {
   Mat w;                   // [F][D / 2] channel-major
@@ -852,16 +857,12 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
   __syncthreads();
   int token[NT], power[NT][2];                                 // fixed point of tokens 2 i and 2 i + 1: 2^hexp h s times 2^power
   float hscale[NT];                                            // 2^hexp of the lane's tokens
-  uint32_t most_scale = 0;                                     // bits of the scale that there is room for; 0: no sums yet
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
     token[i] = min(i * 2 + (g >> 2), B - 1);                   // columns behind the last token: computed, never used
     hscale[i] = pow2(unit_exponent(hm[token[i]]));
+    power[i][0] = power[i][1] = kMaxPower;                     // (sums of nothing)
   }
-  auto power_of = [&](int b) {                                 // (of a product that is rounded: one bit of room; 126: of h that are all 0)
-    const unsigned most = hm[min(b, B - 1)];
-    return min(fixed_exponent(__float_as_uint(__uint_as_float(most) * pow2(unit_exponent(most)) * __uint_as_float(most_scale)) & 0x7fffffffu) + 3, 126);
-  };
 
   int acc[8][NT][4], zacc[NT][4];                              // even columns (rows g): sums of q, odd ones (g + 8): of 16 q
 #pragma unroll
@@ -881,30 +882,57 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
     const float s0 = __half2float(__ushort_as_half((unsigned short)(sw.x >> ((odd >> (r0 * 4) & 1) << 4))));
     const float s1 = __half2float(__ushort_as_half((unsigned short)(sw.y >> ((odd >> (r0 * 4 + 4) & 1) << 4))));
     const bool in0 = tile * 32 + r0 * 4 + t < n, in1 = tile * 32 + r0 * 4 + 4 + t < n;
-    const uint32_t scale_bits = __reduce_max_sync(0xffffffffu, max(__float_as_uint(s0) & 0x7fffffffu, __float_as_uint(s1) & 0x7fffffffu));
-    if (scale_bits > most_scale) {                             // the first tile, seldom another
-      const bool sums = most_scale != 0;
-      most_scale = max(scale_bits, 0x33800000u) + 0x01000000u; // times 4 (at least 2^-24, fp16's least)
+    float x0[NT], x1[NT];                                      // h s as fixed-point numbers
+    auto factor = [&](int i) { return pow2(g < 4 ? power[i][0] : power[i][1]); };
+    auto two_h = [&](int i) { return *reinterpret_cast<const float2*>(st + 2432 + token[i] * 128 + t * 32 + r0 * 4); };
+    float sum = 0.f;                                           // of magnitudes: whether there is room for all, and all are numbers
+    const float s0_in = in0 ? s0 : 0.f, s1_in = in1 ? s1 : 0.f;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const float2 h = two_h(i);
+      x0[i] = h.x * hscale[i] * s0_in * factor(i);
+      x1[i] = h.y * hscale[i] * s1_in * factor(i);
+      sum += fabsf(x0[i]);
+      sum += fabsf(x1[i]);
+    }
+    if (__any_sync(0xffffffffu, !(sum < 1073741824.f))) {      // the first tile, seldom another
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
-        const int old[2] = {power[i][0], power[i][1]};
-        power[i][0] = power_of(2 * i);
-        power[i][1] = power_of(2 * i + 1);
-        if (sums) {                                            // a lane's sums are columns 2 t, 2 t + 1: of one token
-          const int by = min(t & 2 ? old[1] - power[i][1] : old[0] - power[i][0], 62);
-          shift_sums(zacc[i], by, t & 1);
+        const float2 h = two_h(i);                             // (0 where the token does not keep the channel: nothing, whatever the scale)
+        x0[i] = in0 && h.x != 0.f ? h.x * hscale[i] * s0 : 0.f;
+        x1[i] = in1 && h.y != 0.f ? h.y * hscale[i] * s1 : 0.f;
+        // the largest |h s| and |h| of the token's 16 lanes, of the other token's
+        uint32_t most = max(__float_as_uint(x0[i]) & 0x7fffffffu, __float_as_uint(x1[i]) & 0x7fffffffu);
+        uint32_t top = max(in0 ? __float_as_uint(h.x) & 0x7fffffffu : 0u, in1 ? __float_as_uint(h.y) & 0x7fffffffu : 0u);
 #pragma unroll
-          for (int m = 0; m < 8; ++m) shift_sums(acc[m][i], by, t & 1);
+        for (int o = 1; o < 16; o <<= 1) {
+          most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        }
+        const uint32_t most_b = __shfl_xor_sync(0xffffffffu, most, 16), top_b = __shfl_xor_sync(0xffffffffu, top, 16);
+        int by[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const bool same = (b == 0) == (g < 4);
+          const int need = fixed_exponent(same ? most : most_b) + 4;   // below 2^30
+          const int room = max(2, min(2 + (int)(hm[min(2 * i + b, B - 1)] >> 23) - (int)((same ? top : top_b) >> 23), kMaxRoom));
+          by[b] = need < power[i][b] ? power[i][b] - need + room : 0;
+          power[i][b] -= by[b];
+        }
+        x0[i] *= factor(i);
+        x1[i] *= factor(i);
+        if (tile != first && (by[0] | by[1])) {                // a lane's sums are columns 2 t, 2 t + 1: of one token
+          const int mine = min(t & 2 ? by[1] : by[0], 62);
+          shift_sums(zacc[i], mine, t & 1);
+#pragma unroll
+          for (int m = 0; m < 8; ++m) shift_sums(acc[m][i], mine, t & 1);
         }
       }
     }
     uint32_t bf[NT][2];
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      const float2 h = *reinterpret_cast<const float2*>(st + 2432 + token[i] * 128 + t * 32 + r0 * 4);
-      const float v0 = in0 ? h.x * hscale[i] * s0 : 0.f, v1 = in1 ? h.y * hscale[i] * s1 : 0.f;
-      const float factor = pow2(g < 4 ? power[i][0] : power[i][1]);
-      const uint32_t d0 = digits(__float2int_rn(v0 * factor)), d1 = digits(__float2int_rn(v1 * factor));
+      const uint32_t d0 = digits(__float2int_rn(x0[i])), d1 = digits(__float2int_rn(x1[i]));
       // bytes 0, 1 of both numbers, and bytes 2, 3: lanes of digits 0, 1 keep the former and get those of the lane two further on
       const uint32_t low = __byte_perm(d0, d1, 0x5140), high = __byte_perm(d0, d1, 0x7362);   // (d0.0 d1.0 d0.1 d1.1), (.2 .2 .3 .3)
       const uint32_t keep = g & 2 ? high : low, got = __shfl_xor_sync(0xffffffffu, g & 2 ? low : high, 8);
@@ -978,7 +1006,7 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
   for (int i = 0; i < NT; ++i) {
     const int b = i * 2 + (t >> 1);                            // lane t has digits 0, 1 (t even) or 2, 3 (t odd) of the token
     const unsigned most = hm[min(b, B - 1)];
-    const int e = most_scale ? -(t & 2 ? power[i][1] : power[i][0]) - unit_exponent(most) : 0, e0 = max(-126, min(126, e));
+    const int e = -(t & 2 ? power[i][1] : power[i][0]) - unit_exponent(most), e0 = max(-126, min(126, e));
     const float f0 = most >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : pow2(e0), f1 = pow2(max(-126, min(126, e - e0)));
     float* at = red + (size_t)wr * outs + b * width + wc * 128 + g * 16 + (t & 1);
 #pragma unroll

@@ -1,9 +1,9 @@
 """Weights held in 4 bits at the edges of what the calls allow, against the definition in 64 bits.  Tolerances: those of
-tests/test_gpu_w4.py."""
+tests/test_gpu_w4.py, and for the down projection a narrower one (own_reference)."""
 import pytest
 import torch
 
-from tests.test_gpu_w4 import call_ffn, check_ffn, check_linear, ffn_case, ffn_reference, gen, make_w4, tokens
+from tests.test_gpu_w4 import U, call_ffn, check_ffn, check_linear, ffn_case, ffn_reference, gen, input_bound, make_w4, sum_bound, tokens, values
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +45,107 @@ def test_ffn_small_and_large_inputs(pb, powers, zeros):
     ref = ffn_reference(gate, up, down, 128, x, [sel[b].long() for b in range(B)])
     assert (ref[0].abs().amax(1) > 2.0 ** -126).all()
     check_ffn(y, ref, 1)
+
+
+def own_reference(gate, up, down, group, x, kept):
+    """y and a bound in which nothing but a token's own channels counts.  As ffn_reference, but the fixed-point numbers h s are off by
+    2^-24 of the largest |h s| that the token has in the column's group: when the exponent is set, that one takes at least 2^23 of 2^30
+    (6 bits are kept free above it, and an exponent is a whole number), and rounding is off by half a unit.  When the exponent
+    falls, by 3 bits at least, a sum of codes and one of zero points are rounded by half a unit each: 8/7 units of 2^-23 in all, in
+    each of at most 128 warps: 300 times 2^-24."""
+    D = x.shape[1]
+    ys, tols = [], []
+    for b, ids in enumerate(kept):
+        pick = lambda w: tuple(None if t is None else t[ids] for t in w)
+        xd = x[b].double()
+        G, Up, Dn = (values(pick(w), group) for w in (gate, up, down))
+        s = pick(down)[1].double().repeat_interleave(group or D, 1)[:, :D]
+        g, u = G @ xd, Up @ xd
+        dg = sum_bound(D, G.abs() @ xd.abs()) + input_bound(xd[None], G)[0]
+        du = sum_bound(D, Up.abs() @ xd.abs()) + input_bound(xd[None], Up)[0]
+        silu = g / (1 + torch.exp(-g))
+        dsilu = 1.1 * dg + 16 * U * silu.abs() + 2.0 ** -126
+        h = silu * u
+        dh = dsilu * (u.abs() + du) + (silu.abs() + dsilu) * du + 4 * U * h.abs()
+        A = (h.abs() + dh) @ Dn.abs()
+        most = ((h.abs() + dh)[:, None] * s).amax(0)
+        codes = (Dn / s.clamp_min(1e-30)).abs().sum(0)
+        ys.append(h @ Dn)
+        tols.append(dh @ Dn.abs() + 2 * (16 + 8 + 8) * U * A + 2.0 ** -24 * most * (codes + 300))
+    return torch.stack(ys), torch.stack(tols)
+
+
+def with_scales(w, rows, factor):
+    """w with the scales of some rows multiplied (and held to what fp16 has)."""
+    scales = w[1].clone()
+    scales[rows] = (scales[rows].float() * factor).clamp(max=65504).half()
+    return w[0], scales, w[2]
+
+
+def with_scale(w, rows, scale):
+    scales = w[1].clone()
+    scales[rows] = scale
+    return w[0], scales, w[2]
+
+
+@pytest.mark.parametrize("B", [2, 3, 6, 8])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_ffn_channels_of_other_tokens_do_not_count(pb, B, zeros):
+    """Channels that the last token alone keeps have scales up to 2^22 times larger in the down projection: the other tokens' results
+    are as exact as without them."""
+    D, F, k2, group = 512, 1408, 300, 128
+    gate, up, down, x = ffn_case(400 + B, D, F, group, B, zeros)
+    sel = lists(401, B, F, k2)
+    others = torch.zeros(F, dtype=torch.bool, device="cuda")
+    others[sel[:-1].flatten().long()] = True
+    alone = sel[-1][~others[sel[-1].long()]].long()
+    assert len(alone) > 20
+    for factor in (2.0 ** 12, 2.0 ** 22):
+        big = with_scales(down, alone, factor)
+        y = call_ffn(pb, (gate, up, big, x), D, F, group, B, sel, None, k2, 1)
+        check_ffn(y, own_reference(gate, up, big, group, x, [sel[b].long() for b in range(B)]), 1)
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+def test_ffn_skipped_ids_do_not_count(pb, zeros):
+    """Ids that are no channels, in every tile of the list, while channel 0 (which is in no list) has the largest scale that there is."""
+    D, F, k2, group = 512, 1408, 400, 128
+    for B in (1, 4):
+        gate, up, down, x = ffn_case(410 + B, D, F, group, B, zeros)
+        down = with_scale(down, [0], 65504.0)
+        sel = lists(411, B, F - 1, k2) + 1
+        sel[:, ::9], sel[:, 3::31] = -1, F
+        y = call_ffn(pb, (gate, up, down, x), D, F, group, B, sel, None, k2, 1)
+        kept = [sel[b][(sel[b] >= 0) & (sel[b] < F)].long() for b in range(B)]
+        check_ffn(y, own_reference(gate, up, down, group, x, kept), 1)
+
+
+@pytest.mark.parametrize("B", [1, 5])
+@pytest.mark.parametrize("group", [0, 128])
+def test_ffn_large_h_with_a_small_scale(pb, B, group):
+    """Channels whose h is some 2^28 times larger and whose scales in the down projection are 0, and channels whose h is as much larger as
+    their scales are smaller: products, not the largest h times the largest scale, set the precision."""
+    D, F, k2 = 512, 1408, 600
+    gate, up, down, x = ffn_case(420 + B, D, F, group, B, False)
+    loud, quiet = torch.arange(5, F, 97, device="cuda"), torch.arange(11, F, 101, device="cuda")
+    gate = with_scales(gate, loud, 2.0 ** 8)
+    up = with_scales(with_scales(up, loud, 2.0 ** 20), quiet, 2.0 ** 14)
+    down = with_scales(with_scale(down, loud, 0.0), quiet, 2.0 ** -14)
+    sel = lists(421, B, F, k2)
+    y = call_ffn(pb, (gate, up, down, x), D, F, group, B, sel, None, k2, 1)
+    check_ffn(y, own_reference(gate, up, down, group, x, [sel[b].long() for b in range(B)]), 1)
+
+
+@pytest.mark.parametrize("B", [1, 2, 8])
+def test_ffn_products_that_rise_and_fall(pb, B):
+    """Scales of the down projection that grow by 2^30 along the list, fall again, and are 0 for long runs."""
+    D, F, group = 256, 6144, 128
+    gate, up, down, x = ffn_case(430 + B, D, F, group, B, True)
+    j = torch.arange(F, device="cuda")
+    for power in (j / 200.0 - 20, 10 - j / 200.0, (j % 640) / 25.0 - 15):
+        scale = torch.exp2(power.float())[:, None].expand(F, 2).clone()
+        scale[1000:2000] = 0
+        big = (down[0], scale.half(), down[2])
+        sel = j.to(torch.int32).expand(B, F).contiguous()
+        y = call_ffn(pb, (gate, up, big, x), D, F, group, B, sel, None, F, 1)
+        check_ffn(y, own_reference(gate, up, big, group, x, [sel[b].long() for b in range(B)]), 1)
