@@ -363,7 +363,8 @@ prox_status_t prox_rmsnorm(prox_ffn_t* h, const float* x_res_dev, const void* no
  *   zeros   dev uint8 [rows, groups] of 0..16, 16-byte aligned, or NULL: 8 everywhere (symmetric codes)
  * All three are read in place.  A token's inputs enter as fixed-point numbers of 26 bits below its largest, sums over a
  * group are exact, sums of groups fp32; results are the same on every call.  A token with an input that is not finite
- * gets NaN.  Data types are numbered 0 = bf16, 1 = fp32, 2 = fp16.
+ * gets NaN.  A scale that is not finite makes no number of the outputs that it enters, and of no others.  Data types are
+ * numbered 0 = bf16, 1 = fp32, 2 = fp16.
  * Every buffer has to lie on the current device (or in pinned mapped or managed memory); others are refused. */
 typedef struct {
   const uint8_t* codes;
@@ -401,7 +402,10 @@ prox_status_t prox_w4_linear(const prox_w4_t* w, int N, int K, int group_size, c
  *   y                 dev [B, d_model], bf16 (out_dtype 0) or fp32 (1)
  *   workspace         dev, 16-byte aligned, at least prox_w4_stage2_workspace bytes; its contents mean nothing before
  *                     or after a call, but calls that may overlap need one each
- * For B > 1 the weights are read once for the union of the tokens' masks.
+ * For B > 1 the weights are read once for the union of the tokens' masks.  A token's y depends on the channels that it
+ * keeps alone.  h is fp32; h times a scale of the down projection is a fixed-point number, off by 2^-24 of the token's
+ * largest such product at most, and sums of those are exact in a warp and fp32 between warps.  A scale of the down
+ * projection that is not finite makes NaN of y in its group's columns, for the tokens that keep the channel with an h other than 0.
  * Errors: INVALID_ARG, UNSUPPORTED (shape, group_size), CUDA. */
 prox_status_t prox_w4_stage2_workspace(int d_model, int d_ff, int B, int64_t* bytes);
 prox_status_t prox_w4_stage2_ffn(const prox_w4_t* gate, const prox_w4_t* up, const prox_w4_t* down_t, int d_model,

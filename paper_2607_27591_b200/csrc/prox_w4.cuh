@@ -914,7 +914,7 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
           const bool same = (b == 0) == (g < 4);
-          const int need = fixed_exponent(same ? most : most_b) + 4;   // below 2^30
+          const int need = fixed_exponent(same ? most : most_b) + 4;   // below 2^30 (11 at least; -99 for what is not finite)
           const int room = max(2, min(2 + (int)(hm[min(2 * i + b, B - 1)] >> 23) - (int)((same ? top : top_b) >> 23), kMaxRoom));
           by[b] = need < power[i][b] ? power[i][b] - need + room : 0;
           power[i][b] -= by[b];
@@ -1006,8 +1006,9 @@ __global__ void __launch_bounds__(down_threads(NT), 1) down_kernel(const DownArg
   for (int i = 0; i < NT; ++i) {
     const int b = i * 2 + (t >> 1);                            // lane t has digits 0, 1 (t even) or 2, 3 (t odd) of the token
     const unsigned most = hm[min(b, B - 1)];
-    const int e = -(t & 2 ? power[i][1] : power[i][0]) - unit_exponent(most), e0 = max(-126, min(126, e));
-    const float f0 = most >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : pow2(e0), f1 = pow2(max(-126, min(126, e - e0)));
+    const int fixed = t & 2 ? power[i][1] : power[i][0], e = -fixed - unit_exponent(most), e0 = max(-126, min(126, e));
+    // (a fixed point below 0: some product was not finite)
+    const float f0 = most >= 0x7f800000u || fixed < 0 ? __uint_as_float(0x7fffffffu) : pow2(e0), f1 = pow2(max(-126, min(126, e - e0)));
     float* at = red + (size_t)wr * outs + b * width + wc * 128 + g * 16 + (t & 1);
 #pragma unroll
     for (int m = 0; m < 8; ++m) {                              // columns g * 16 + 2 m (even lanes), + 1 (odd lanes) of the warp's

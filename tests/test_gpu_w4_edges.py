@@ -149,3 +149,59 @@ def test_ffn_products_that_rise_and_fall(pb, B):
         sel = j.to(torch.int32).expand(B, F).contiguous()
         y = call_ffn(pb, (gate, up, big, x), D, F, group, B, sel, None, F, 1)
         check_ffn(y, own_reference(gate, up, big, group, x, [sel[b].long() for b in range(B)]), 1)
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("B", [1, 2, 3, 8])
+def test_ffn_a_scale_that_is_not_finite_stays_with_its_tokens(pb, B, bad):
+    """A scale of the down projection that is not finite makes NaN of the outputs of its column group, for the tokens that keep its channel;
+    no other output changes.  In a channel of one token, in one of all, and in channel 0 where it stands for skipped ids."""
+    D, F, k2, group = 512, 1408, 300, 128
+    gate, up, down, x = ffn_case(440 + B, D, F, group, B, B == 3)
+    sel = lists(441, B, F - 1, k2) + 1
+    sel[:, 7] = -1                                               # ids that are skipped
+    kept = [sel[b][sel[b] >= 0].long() for b in range(B)]
+    plain = call_ffn(pb, (gate, up, down, x), D, F, group, B, sel, None, k2, 1)
+    check_ffn(plain, own_reference(gate, up, down, group, x, kept), 1)
+    some = [ids[ids % 7 != 0] for ids in kept]                   # (of every seventh channel the gate's scales are 0, and so is h)
+    for channel in (0, int(some[-1][100]), int(some[0][-1])):
+        broken = with_scale(down, (channel, 2), bad)
+        y = call_ffn(pb, (gate, up, broken, x), D, F, group, B, sel, None, k2, 1)
+        ref, tol = own_reference(gate, up, down, group, x, kept)
+        for b in range(B):
+            hit = bool((kept[b] == channel).any())
+            assert torch.isnan(y[b, 256:384]).all() == hit, (channel, b)
+            rest = torch.cat((torch.arange(256), torch.arange(384 if hit else 256, D)))
+            check_ffn(y[b:b + 1, rest], (ref[b:b + 1, rest], tol[b:b + 1, rest]), 1)
+
+
+@pytest.mark.parametrize("B", [1, 4])
+def test_ffn_a_gate_scale_that_is_not_finite_stays_with_its_tokens(pb, B):
+    D, F, k2, group = 512, 1408, 300, 128
+    gate, up, down, x = ffn_case(450 + B, D, F, group, B, False)
+    sel = lists(451, B, F, k2)
+    channel = int(sel[-1][sel[-1] % 7 != 0][9])
+    for w in (0, 1):
+        m = [gate, up]
+        m[w] = with_scale(m[w], (channel, 1), float("inf"))
+        y = call_ffn(pb, (*m, down, x), D, F, group, B, sel, None, k2, 1)
+        for b in range(B):
+            if bool((sel[b] == channel).any()):
+                assert not torch.isfinite(y[b]).any()
+            else:
+                check_ffn(y[b:b + 1], own_reference(gate, up, down, group, x[b:b + 1], [sel[b].long()]), 1)
+
+
+def test_linear_inputs_that_are_not_finite(pb):
+    """One input that is not finite, anywhere in a token: all of the token's outputs are NaN, whatever the scales; one block and clusters."""
+    for N, K, group in ((272, 512, 128), (40, 14336, 128), (3000, 4096, 32)):
+        B = 5
+        w = make_w4(N, N, K, group, False, spread=0.01)
+        for at in (0, K // 2 + 3, K - 1):
+            x = tokens(N, B, K, torch.bfloat16)
+            x[1, at], x[3, at] = float("inf"), float("nan")
+            x[4] = float("-inf")
+            y = torch.empty(B, N, device="cuda")
+            pb.prox_w4_linear(w, N, K, group, x, K, 0, B, y, N, 1)
+            assert torch.isnan(y[[1, 3, 4]]).all()
+            check_linear(y[[0, 2]], w, group, x[[0, 2]], K, 1)
