@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "prox.h"
 
 cudaError_t prox_noalloc_load(int device);
@@ -27,14 +29,19 @@ inline bool host_on_current_device(const void* p, int device) {
   return at.type == cudaMemoryTypeManaged || (at.type == cudaMemoryTypeHost && at.devicePointer == p);
 }
 
+// Facts about a device that are asked for once and kept (threads that ask at the same time find the same).
+constexpr int kKnownDevices = 64;
+
 inline int host_sm_count(int device) {
-  static int known[64] = {};                       // the same value whoever writes it
-  int& n = known[device & 63];
-  if (n < 1 && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) {
+  static std::atomic<int> known[kKnownDevices];
+  std::atomic<int>* at = device < kKnownDevices ? known + device : nullptr;
+  int n = at ? at->load(std::memory_order_relaxed) : 0;
+  if (n > 0) return n;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || n < 1) {
     (void)cudaGetLastError();
-    n = 0;
     return 148;
   }
+  if (at) at->store(n, std::memory_order_relaxed);
   return n;
 }
 
@@ -56,10 +63,11 @@ constexpr int kMaxBlockSmem = 227 * 1024;
 // Lets a kernel with dynamic shared memory have that of a whole SM (once per device).
 template <auto Kern>
 cudaError_t host_allow_smem(int device) {
-  static bool allowed[64] = {};
-  if (allowed[device & 63]) return cudaSuccess;
+  static std::atomic<bool> allowed[kKnownDevices];
+  std::atomic<bool>* at = device < kKnownDevices ? allowed + device : nullptr;
+  if (at && at->load(std::memory_order_acquire)) return cudaSuccess;
   const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(Kern), cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxBlockSmem - 8192);
-  if (e == cudaSuccess) allowed[device & 63] = true;
+  if (e == cudaSuccess && at) at->store(true, std::memory_order_release);
   return e;
 }
 

@@ -3,6 +3,7 @@
 #include "prox_w4.cuh"
 
 #include <algorithm>
+#include <atomic>
 
 using namespace prox;
 
@@ -16,8 +17,9 @@ constexpr int kFfnTokens = 8;            // tokens of a call of the sparse FFN, 
 // Clusters of S blocks that the GPU holds at once (a block of these kernels has an SM to itself).
 template <auto Kern>
 int clusters_at_once(int device, int S, int threads, size_t smem) {
-  static int known[64][9] = {};
-  int& n = known[device & 63][S];
+  static std::atomic<int> known[kKnownDevices][9];
+  std::atomic<int>* kept = device < kKnownDevices ? &known[device][S] : nullptr;
+  int n = kept ? kept->load(std::memory_order_relaxed) : 0;
   if (n > 0) return n;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(S); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem;
@@ -29,6 +31,7 @@ int clusters_at_once(int device, int S, int threads, size_t smem) {
     (void)cudaGetLastError();
     n = std::max(1, 128 / S);
   }
+  if (kept) kept->store(n, std::memory_order_relaxed);
   return n;
 }
 
