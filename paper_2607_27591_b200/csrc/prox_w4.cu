@@ -84,7 +84,7 @@ FfnWorkspace ffn_workspace(int F, int B) {
 }
 
 template <int NT, bool ZP>
-cudaError_t launch_down(w4::DownArgs& a, int dev, cudaStream_t st) {
+cudaError_t launch_down(w4::DownArgs& a, int sms, int dev, cudaStream_t st) {
   constexpr int kThreads = w4::down_threads(NT), kWarps = kThreads / 32;
   constexpr auto kern = w4::down_kernel<NT, ZP>;
   const int cgs = a.D / 128, tiles = std::max(1, (a.n + 31) / 32);
@@ -93,7 +93,7 @@ cudaError_t launch_down(w4::DownArgs& a, int dev, cudaStream_t st) {
   double least = 1e30;
   for (int S = 8; S >= 1; S /= 2)
     for (int WC = 8; WC >= 1; WC /= 2) {
-      const int slices = (cgs + WC - 1) / WC, at_once = S == 1 ? 148 : clusters_at_once<kern>(dev, S, kThreads, smem);
+      const int slices = (cgs + WC - 1) / WC, at_once = S == 1 ? sms : clusters_at_once<kern>(dev, S, kThreads, smem);
       const int waves = (slices + at_once - 1) / at_once, rounds = ((tiles + S - 1) / S + kWarps / WC - 1) / (kWarps / WC);
       if (tiles > 1024 * S) continue;                          // (32768 entries a block: its sums stay below 2^31)
       const double cost = waves * (rounds + 2.0) + (S > 1 ? 1.0 : 0.0) - 0.01 * WC;
@@ -103,8 +103,8 @@ cudaError_t launch_down(w4::DownArgs& a, int dev, cudaStream_t st) {
 }
 
 template <int NT>
-cudaError_t launch_down(w4::DownArgs& a, int dev, cudaStream_t st) {
-  return a.w.zeros ? launch_down<NT, true>(a, dev, st) : launch_down<NT, false>(a, dev, st);
+cudaError_t launch_down(w4::DownArgs& a, int sms, int dev, cudaStream_t st) {
+  return a.w.zeros ? launch_down<NT, true>(a, sms, dev, st) : launch_down<NT, false>(a, sms, dev, st);
 }
 
 template <int W, bool ZP, bool GATEUP>
@@ -248,8 +248,8 @@ prox_status_t prox_w4_stage2_ffn(const prox_w4_t* gate, const prox_w4_t* up, con
   d.D = D; d.F = F; d.groups = groups; d.gstep = group_size != 0;
   d.list = list; d.count = count; d.n = most; d.h = h; d.B = B; d.y = y_dev; d.y_type = out_dtype;
   d.hmax = a.hmax; d.hblocks = p.grid;
-  CKL(nt == 1 ? launch_down<1>(d, dev, st) : nt == 2 ? launch_down<2>(d, dev, st) : nt == 3 ? launch_down<3>(d, dev, st)
-                                                                                                      : launch_down<4>(d, dev, st));
+  CKL(nt == 1 ? launch_down<1>(d, sms, dev, st) : nt == 2 ? launch_down<2>(d, sms, dev, st) : nt == 3 ? launch_down<3>(d, sms, dev, st)
+                                                                                                     : launch_down<4>(d, sms, dev, st));
   return PROX_OK;
 }
 
