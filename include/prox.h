@@ -361,8 +361,9 @@ prox_status_t prox_rmsnorm(prox_ffn_t* h, const float* x_res_dev, const void* no
  *   codes   dev uint8 [rows, cols / 2], 16-byte aligned: byte i holds column 2i in bits 0-3, column 2i + 1 in bits 4-7
  *   scales  dev fp16 [rows, groups], groups = ceil(cols / G) (the last group may be shorter), 16-byte aligned
  *   zeros   dev uint8 [rows, groups] of 0..16, 16-byte aligned, or NULL: 8 everywhere (symmetric codes)
- * All three are read in place.  A token's inputs enter as fixed-point numbers of 26 bits below its largest, sums over a
- * group are exact, sums of groups fp32; results are the same on every call.  A token with an input that is not finite
+ * All three are read in place.  A token's inputs enter as fixed-point numbers of 26 bits below its largest: off by
+ * 2^-26 of that at most (bf16 inputs from 2^-18 of it on are exact, fp16 ones from 2^-15 on), so an output is off by
+ * 2^-26 max|x| sum|w| beside fp32's own rounding.  Sums over a group are exact, sums of groups fp32; results are the same on every call.  A token with an input that is not finite
  * gets NaN.  A scale that is not finite makes no number of the outputs that it enters, and of no others.  Data types are
  * numbered 0 = bf16, 1 = fp32, 2 = fp16.
  * Every buffer has to lie on the current device (or in pinned mapped or managed memory); others are refused. */
@@ -383,7 +384,7 @@ prox_status_t prox_w4_quantize(const void* w_dev, int rows, int cols, int group_
  *   x  dev bf16 or fp16 (x_dtype) [B, K], rows x_stride elements apart (any alignment of the type's size)
  *   y  dev bf16, fp32 or fp16 (y_dtype) [B, N], rows y_stride elements apart; what lies between rows stays
  * K is a multiple of 32, at most 65536; N and B are any numbers from 1; strides matter for B > 1 only.
- * The weights are read once for up to 8 tokens (fewer for very long rows), again for the next 8: a call for a
+ * The weights are read once for up to 8 tokens (fewer for long rows), again for the next 8: a call for a
  * few tokens, not for a prompt.  y must not overlap x.  Errors: INVALID_ARG, UNSUPPORTED (K, group_size), CUDA. */
 prox_status_t prox_w4_linear(const prox_w4_t* w, int N, int K, int group_size, const void* x_dev, int64_t x_stride,
                              int x_dtype, int B, void* y_dev, int64_t y_stride, int y_dtype, void* stream);
